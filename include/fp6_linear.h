@@ -69,7 +69,9 @@ typedef enum {
     FP6_ERR_WORKSPACE = -4,  /* workspace missing or too small for every plan of the call    */
     FP6_ERR_VARIANT = -5,    /* kernel variant / split request not valid for this shape      */
     FP6_ERR_HIP = -6,        /* the HIP runtime reported a launch error                      */
-    FP6_ERR_SCRATCH = -7     /* fp6_linear_static: the shape needs more than its built-in scratch */
+    FP6_ERR_SCRATCH = -7,    /* fp6_linear_static: the shape needs more than its built-in scratch */
+    FP6_ERR_OVERLAP = -8,    /* a buffer that is written overlaps another one                */
+    FP6_ERR_VALUE = -9       /* a type, rank, count or other number is outside what the call takes */
 } fp6_status;
 
 /* kernel families behind fp6_linear (see fp6_linear_variant) */
@@ -387,6 +389,127 @@ int fp6_linear_v2(const uint16_t *X, int64_t M, const void *hi_plane, const void
 int fp6_linear_v2_bf16(const uint16_t *X, int64_t M, const void *hi_plane, const void *lo_plane,
                        const uint16_t *scales, int64_t N, int64_t K, uint16_t *Y,
                        void *workspace, size_t workspace_bytes, void *stream, int variant, int split_k);
+
+/*
+ * ---- Around the frozen layer: low-rank adapters, the layer's gradient, the adapters' update
+ *
+ * The weights of the layer stay as they are; what is trained, and what differs from request to request, are adapters beside it.
+ * These calls keep the conventions above (caller-owned device buffers, 16-byte aligned; asynchronous on `stream`; argument errors
+ * found on the host; N and K multiples of 64).  `type` is the type of the 16-bit tensors of a call.
+ */
+#define FP6_F16 0
+#define FP6_BF16 1
+#define FP6_F32 2                /* gradients of fp6_adamw */
+#define FP6_NO_COPY (-1)         /* fp6_adamw: no 16-bit copies */
+#define FP6_LORA_RANK_MAX 128
+
+/*
+ * Low-rank adapters of many requests beside a shared projection: with a = index[m] the adapter of row m,
+ *     out[m,:] = round(Y[m,:] + scaling[a] * (X[m,:] A[a]^T) B[a]^T)
+ * added in fp32 and rounded once; Y is what the projection gave (any linear call of this library).  X A^T is kept in fp32 between
+ * the two products and enters the second one as two 16-bit terms (22 bits with fp16, 16 with bf16).
+ *   X       [M,K]            A   [adapters, rank, K]        B   [adapters, N, rank]        Y, out   [M,N]; out may be Y
+ *   hidden  fp32 [M,rank] or NULL: X A^T (without scaling), which fp6_lora_backward wants; zeros in rows without an adapter
+ *   index   int32 [M] on the device, or NULL: adapter 0 for every row.  A value outside 0 .. adapters-1 means no adapter: the row
+ *           of out is the row of Y, bit for bit, whatever X holds there.  Rows may come in any order; rows of one adapter
+ *           that are neighbours are cheapest.
+ *   scaling fp32 [adapters] on the device, or NULL: 1
+ *   rank    8 .. FP6_LORA_RANK_MAX, a multiple of 8 (adapters of a lower rank: rows of zeros)
+ *   workspace  >= fp6_lora_workspace_bytes; the contract of fp6_linear's workspace: its first FP6_WORKSPACE_ZERO_BYTES bytes are
+ *           left as they are (so one buffer serves both), the rest need not be zero.  Calls that share it must not overlap in time.
+ * fp6_lora_group: up to FP6_GROUP_MAX projections of the same rows (q, k and v; gate and up) in the same two launches; the rows'
+ * adapters and the scaling are common, N, K and rank may differ.  No out may overlap what another layer of the group reads.
+ * An infinity or NaN in a row of X stays in that row.  Errors: FP6_ERR_NULL, FP6_ERR_SHAPE, FP6_ERR_ALIGN, FP6_ERR_VALUE (type,
+ * rank, adapters), FP6_ERR_OVERLAP, FP6_ERR_WORKSPACE, FP6_ERR_HIP.
+ */
+typedef struct fp6_lora_problem {
+    const uint16_t *X, *A, *B, *Y;
+    uint16_t *out;
+    float *hidden;
+    int64_t N, K, rank;
+} fp6_lora_problem;
+size_t fp6_lora_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t rank, int64_t adapters);
+int fp6_lora(int type, const uint16_t *X, int64_t M, const uint16_t *A, const uint16_t *B, int64_t adapters, int64_t rank,
+             const int32_t *index, const float *scaling, const uint16_t *Y, int64_t N, int64_t K, uint16_t *out, float *hidden,
+             void *workspace, size_t workspace_bytes, void *stream);
+size_t fp6_lora_group_workspace_bytes(int64_t M, const fp6_lora_problem *problems, int count, int64_t adapters);
+int fp6_lora_group(int type, int64_t M, const fp6_lora_problem *problems, int count, int64_t adapters, const int32_t *index,
+                   const float *scaling, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The gradients of fp6_lora for the gradient dY [M,N] of its result:
+ *     dH[m,:] = scaling[a] * dY[m,:] B[a]                      out[m,:] = round(dX[m,:] + dH[m,:] A[a])
+ *     dA[a]   = sum over the rows of a of dH[m,:]^T X[m,:]     dB[a]   = sum over the rows of a of scaling[a] dY[m,:]^T hidden[m,:]
+ *   dX, out  [M,K] 16 bits: dX is the gradient that reached X by other ways (fp6_linear_grad's result), out may be dX; both NULL:
+ *            no gradient for X is wanted.  Rows without an adapter: out is dX, bit for bit, and they enter no sum, whatever they hold.
+ *   dA, dB   fp32 [adapters, rank, K] and [adapters, N, rank]; accumulate != 0 adds to them, else adapters without rows get zeros
+ *   hidden   as fp6_lora left it
+ * The sums are fp32 in an order that depends on the sizes only: two calls give the same bits.
+ */
+size_t fp6_lora_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t rank, int64_t adapters);
+int fp6_lora_backward(int type, const uint16_t *dY, const uint16_t *X, const float *hidden, int64_t M, const uint16_t *A,
+                      const uint16_t *B, int64_t adapters, int64_t rank, const int32_t *index, const float *scaling,
+                      const uint16_t *dX, uint16_t *out, float *dA, float *dB, int accumulate, int64_t N, int64_t K,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The gradient of a frozen layer by its input: dX[m,k] = sum_n dY[m,n] * S_n * value(code[n,k]).  The weight is packed a second
+ * time for it, turned, once (0.75 byte a weight, FP5 0.625), and the layer's own kernels compute the product.
+ *   format   FP6_FORMAT_E3M2 (planes of fp6_quantize_pack), FP6_FORMAT_E3M1 (fp5_quantize_pack), FP6_FORMAT_E3M2_V2 and
+ *            FP6_FORMAT_E3M2_V2_BF16 (fp6_quantize_pack_v2; dY and dX fp16, or bf16).  Row scales only: fine-grained scales
+ *            stand neither beside the sum nor beside dY.
+ *   hi_t, lo_t   planes of the [K,N] codes, as large as those of [N,K], same layout
+ *   scales_t     fp16 [K]: 2^E, the power of two at or above the largest S_n (at most 2^15)
+ *   ratio        fp32 [N]: S_n / 2^E
+ * fp6_linear_grad rounds dY * ratio to the type of dY, sums in fp32 and rounds the result: twice the rounding error of the result alone
+ * in the mean square.  workspace: >= fp6_linear_grad_workspace_bytes, contract as for fp6_linear (its first
+ * FP6_WORKSPACE_ZERO_BYTES bytes zero before first use, left zero).  FP6_ERR_VARIANT: another format.
+ */
+int fp6_transpose_pack(int format, const void *hi_plane, const void *lo_plane, const uint16_t *scales, int64_t N, int64_t K,
+                       void *hi_t, void *lo_t, uint16_t *scales_t, float *ratio, void *stream);
+size_t fp6_linear_grad_workspace_bytes(int format, int64_t M, int64_t N, int64_t K);
+int fp6_linear_grad(int format, const uint16_t *dY, int64_t M, const void *hi_t, const void *lo_t, const uint16_t *scales_t,
+                    const float *ratio, int64_t N, int64_t K, uint16_t *dX, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One AdamW step over many tensors in one launch (t = *step + 1):
+ *     g = grad_scale * grad     m = b1 m + (1 - b1) g     v = b2 v + (1 - b2) g^2
+ *     param = param (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)     copy = round(param)
+ * in fp32, every operation rounded once, in this order; 1 - lr wd, lr / (1 - b1^t) and 1 / sqrt(1 - b2^t) are taken in double.
+ *   state_bits 32: first and second are m and v, fp32.  8: first and second are m and sqrt(v) as e4m3 bytes (largest 448), one
+ *     scale byte e per 256 elements in first_scales and second_scales (ceil(count / 256) of them): value = code * 2^(e-127), the
+ *     smallest such power that brings the block to 448 or below; all bytes zero is the state zero.  The last kept bit is
+ *     rounded up with the probability that makes the rounding unbiased, by a hash of the element's number, t and `seed` (the
+ *     numbers run through the tensors of the plan, each starting at a multiple of 256); a nonzero sqrt(v) never becomes zero.
+ *   grad_type FP6_F32, FP6_F16 or FP6_BF16; copy_type FP6_F16, FP6_BF16 or FP6_NO_COPY: one of each for all tensors of a plan.
+ *   step      int32 on the device, the steps done so far; the call adds one.
+ * fp6_adamw_plan writes, on the host, what the kernel needs of the tensors into plan_host (fp6_adamw_plan_bytes bytes); the
+ * caller copies it to 16-byte aligned device memory once and keeps it as long as the tensors stay where they are.  It refuses
+ * NULL (FP6_ERR_NULL), misaligned (16 bytes; scale bytes: any; FP6_ERR_ALIGN) and overlapping (FP6_ERR_OVERLAP: what is
+ * written twice, or written and read as a gradient) tensors; a count of 0 is fine.  `items` receives what fp6_adamw wants to know.
+ * One call at a time may use a plan.  lr may come from the device (lr_device != NULL: it counts instead of lr), as may grad_scale
+ * (NULL: 1; the inverse of a loss scale, a clipping factor); found_inf (NULL: never): where it is not 0 the call changes nothing,
+ * not even step.  So a captured call can be replayed as step, learning rate and scale move on.
+ * FP6_ERR_VALUE: beta outside [0, 1), negative or non-finite lr, eps or weight_decay, state_bits, types, items.
+ */
+typedef struct fp6_adamw_tensor {
+    float *param;
+    const void *grad;
+    void *first, *second;
+    uint8_t *first_scales, *second_scales;     /* state_bits 8 */
+    uint16_t *copy;                            /* unless copy_type is FP6_NO_COPY */
+    int64_t count;
+} fp6_adamw_tensor;
+typedef struct fp6_adamw_options {
+    double lr, beta1, beta2, eps, weight_decay;
+    const float *lr_device, *grad_scale, *found_inf;
+    uint32_t seed;
+} fp6_adamw_options;
+size_t fp6_adamw_plan_bytes(const fp6_adamw_tensor *tensors, int64_t count);
+int fp6_adamw_plan(const fp6_adamw_tensor *tensors, int64_t count, int state_bits, int grad_type, int copy_type, void *plan_host,
+                   size_t plan_bytes, int64_t *items);
+int fp6_adamw(void *plan, int64_t items, int state_bits, int grad_type, int copy_type, int32_t *step,
+              const fp6_adamw_options *options, void *stream);
 
 /*
  * Measurement aids (no passage of the paper: they measure the chip, not the method).  Each

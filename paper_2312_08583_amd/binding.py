@@ -63,7 +63,10 @@ EXPORTS = ["fp6_layout_version", "fp6_status_string", "fp6_packed_sizes", "fp6_q
            "fp5_quantize_pack", "fp5_unpack_codes", "fp5_dequantize", "fp5_linear_workspace_bytes", "fp5_linear",
            "fp6_quantize_pack_v2", "fp6_unpack_codes_v2", "fp6_dequantize_v2", "fp6_linear_v2_workspace_bytes",
            "fp6_linear_v2", "fp6_linear_v2_bf16", "fp6_probe_read", "fp6_probe_mfma", "fp6_linear_plan", "fp6_linear_static", "fp6_linear_group",
-           "fp6_linear_group_workspace_bytes"]
+           "fp6_linear_group_workspace_bytes",
+           "fp6_lora_workspace_bytes", "fp6_lora", "fp6_lora_group_workspace_bytes", "fp6_lora_group",
+           "fp6_lora_backward_workspace_bytes", "fp6_lora_backward", "fp6_transpose_pack", "fp6_linear_grad_workspace_bytes",
+           "fp6_linear_grad", "fp6_adamw_plan_bytes", "fp6_adamw_plan", "fp6_adamw"]
 
 FP6_FORMAT_E3M2, FP6_FORMAT_E3M1, FP6_FORMAT_E3M2_V2, FP6_FORMAT_E3M2_V2_BF16 = 6, 5, 7, 8
 
@@ -82,6 +85,31 @@ class PlanInfo(ctypes.Structure):
     _fields_ = [("variant", ctypes.c_int), ("split_k", ctypes.c_int), ("block_m", ctypes.c_int), ("width", ctypes.c_int),
                 ("waves", ctypes.c_int), ("depth", ctypes.c_int), ("half_tiles", ctypes.c_int), ("meeting", ctypes.c_int),
                 ("workgroups", ctypes.c_int64), ("workspace_bytes", ctypes.c_size_t)]
+
+
+
+FP6_F16, FP6_BF16, FP6_F32, FP6_NO_COPY = 0, 1, 2, -1
+FP6_LORA_RANK_MAX = 128
+
+
+class LoraProblem(ctypes.Structure):
+    """fp6_lora_problem of the header."""
+    _fields_ = [("X", ctypes.c_void_p), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("Y", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("hidden", ctypes.c_void_p), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
+                ("rank", ctypes.c_int64)]
+
+
+class AdamWTensor(ctypes.Structure):
+    """fp6_adamw_tensor of the header."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "first", "second", "first_scales", "second_scales", "copy")] + \
+        [("count", ctypes.c_int64)]
+
+
+class AdamWOptions(ctypes.Structure):
+    """fp6_adamw_options of the header."""
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
+        [(n, ctypes.c_void_p) for n in ("lr_device", "grad_scale", "found_inf")] + [("seed", ctypes.c_uint32)]
+
 
 _LIB = None
 
@@ -194,6 +222,30 @@ def lib() -> ctypes.CDLL:
     L.fp6_linear_group_workspace_bytes.argtypes = [i64, ctypes.POINTER(LinearProblem), ci]
     L.fp6_linear_group.restype = ci
     L.fp6_linear_group.argtypes = [i64, ctypes.POINTER(LinearProblem), ci, p, sz, p]
+    L.fp6_lora_workspace_bytes.restype = sz
+    L.fp6_lora_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    L.fp6_lora.restype = ci
+    L.fp6_lora.argtypes = [ci, p, i64, p, p, i64, i64, p, p, p, i64, i64, p, p, p, sz, p]
+    L.fp6_lora_group_workspace_bytes.restype = sz
+    L.fp6_lora_group_workspace_bytes.argtypes = [i64, ctypes.POINTER(LoraProblem), ci, i64]
+    L.fp6_lora_group.restype = ci
+    L.fp6_lora_group.argtypes = [ci, i64, ctypes.POINTER(LoraProblem), ci, i64, p, p, p, sz, p]
+    L.fp6_lora_backward_workspace_bytes.restype = sz
+    L.fp6_lora_backward_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    L.fp6_lora_backward.restype = ci
+    L.fp6_lora_backward.argtypes = [ci, p, p, p, i64, p, p, i64, i64, p, p, p, p, p, p, ci, i64, i64, p, sz, p]
+    L.fp6_transpose_pack.restype = ci
+    L.fp6_transpose_pack.argtypes = [ci, p, p, p, i64, i64, p, p, p, p, p]
+    L.fp6_linear_grad_workspace_bytes.restype = sz
+    L.fp6_linear_grad_workspace_bytes.argtypes = [ci, i64, i64, i64]
+    L.fp6_linear_grad.restype = ci
+    L.fp6_linear_grad.argtypes = [ci, p, i64, p, p, p, p, i64, i64, p, p, sz, p]
+    L.fp6_adamw_plan_bytes.restype = sz
+    L.fp6_adamw_plan_bytes.argtypes = [ctypes.POINTER(AdamWTensor), i64]
+    L.fp6_adamw_plan.restype = ci
+    L.fp6_adamw_plan.argtypes = [ctypes.POINTER(AdamWTensor), i64, ci, ci, ci, p, sz, ctypes.POINTER(i64)]
+    L.fp6_adamw.restype = ci
+    L.fp6_adamw.argtypes = [p, i64, ci, ci, ci, p, ctypes.POINTER(AdamWOptions), p]
     L.fp6_linear_plan.restype = ci
     L.fp6_linear_plan.argtypes = [ci, i64, i64, i64, i64, ci, ci, ctypes.POINTER(PlanInfo)]
     _LIB = L
@@ -566,6 +618,256 @@ def fp6_linear_v2_bf16(X: torch.Tensor, hi: torch.Tensor, lo: torch.Tensor, scal
     need = lambda M: fp6_linear_v2_workspace_bytes(M, N, K, variant, split_k)
     return _linear("fp6_linear_v2_bf16", need, X, hi, lo, scales, N, K, out, workspace, (variant, split_k),
                    dtype=torch.bfloat16)
+
+
+# ---- low-rank adapters beside the frozen layer, its gradient, the adapters' update
+
+_TYPE = {torch.float16: FP6_F16, torch.bfloat16: FP6_BF16, torch.float32: FP6_F32}
+
+
+class _Call:
+    """Pointers of a call's tensors, all checked to lie on one device; the launch goes to that device's current stream."""
+
+    def __init__(self, first: torch.Tensor, what: str):
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+            raise Fp6Error("%s must be a GPU tensor (this library has no CPU path)" % what)
+        self.device = first.device
+
+    def ptr(self, t: torch.Tensor, dtype, what: str, shape=None) -> int:
+        p = _dev(t, dtype, what)
+        if t.device != self.device:
+            raise Fp6Error("%s is on %s, the call's other tensors on %s" % (what, t.device, self.device))
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            raise Fp6Error("%s must be %s, got %s" % (what, list(shape), list(t.shape)))
+        return p
+
+    def flat(self, t: torch.Tensor, dtype, what: str, numel: int) -> int:
+        p = self.ptr(t, dtype, what)
+        if t.numel() != numel:
+            raise Fp6Error("%s holds %d elements, the shape needs %d" % (what, t.numel(), numel))
+        return p
+
+    def optional(self, t, dtype, what: str, shape=None):
+        return None if t is None else self.ptr(t, dtype, what, shape)
+
+    def workspace(self, t, need):
+        """Pointer, bytes and the tensor to keep until the launch."""
+        if t is None:
+            t = new_workspace(int(need()), self.device)
+        if t is None:
+            return None, 0, None
+        return self.ptr(t, torch.uint8, "workspace"), t.numel(), t
+
+    def launch(self, name: str, *args) -> None:
+        with torch.cuda.device(self.device):
+            _check(getattr(lib(), name)(*args, _stream()), name)
+
+
+def _adapters(call: _Call, X, A, B):
+    """Pointers of A [adapters, rank, K] and B [adapters, N, rank] and their sizes, X [M,K] known to the caller."""
+    if not isinstance(X, torch.Tensor) or X.dtype not in (torch.float16, torch.bfloat16):
+        raise Fp6Error("X must be fp16 or bf16")
+    if not isinstance(A, torch.Tensor) or not isinstance(B, torch.Tensor) or A.dim() != 3 or B.dim() != 3:
+        raise Fp6Error("A must be [adapters,rank,K] and B [adapters,N,rank]")
+    L, rank, K = A.shape
+    N = B.shape[1]
+    if X.dim() != 2 or X.shape[1] != K or X.shape[0] < 1:
+        raise Fp6Error("X must be [M,K] = [M,%d] with M >= 1" % K)
+    if rank < 8 or rank > FP6_LORA_RANK_MAX or rank % 8:
+        raise Fp6Error("rank must be a multiple of 8 from 8 to %d (a lower one: rows of zeros)" % FP6_LORA_RANK_MAX)
+    if L < 1:
+        raise Fp6Error("no adapter")
+    _shape_ok(N, K)
+    return call.ptr(A, X.dtype, "A"), call.ptr(B, X.dtype, "B", (L, N, rank)), L, rank, N, K
+
+
+def fp6_lora_workspace_bytes(M: int, N: int, K: int, rank: int, adapters: int = 1) -> int:
+    return int(lib().fp6_lora_workspace_bytes(M, N, K, rank, adapters))
+
+
+def fp6_lora(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, Y: torch.Tensor, index: Optional[torch.Tensor] = None,
+             scaling: Optional[torch.Tensor] = None, hidden: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[m] = Y[m] + scaling[a] (X[m] A[a]^T) B[a]^T with a = index[m]; without `out` into Y itself.
+
+    X [M,K], Y [M,N], A [adapters,rank,K], B [adapters,N,rank], all fp16 or all bf16; index int32 [M] (None: adapter 0; outside
+    the adapters: none, the row of Y stays); scaling fp32 [adapters]; hidden fp32 [M,rank] receives X A^T."""
+    call = _Call(X, "X")
+    a, b, L, rank, N, K = _adapters(call, X, A, B)
+    M = X.shape[0]
+    out = Y if out is None else out
+    ws, wb, workspace = call.workspace(workspace, lambda: fp6_lora_workspace_bytes(M, N, K, rank, L))
+    call.launch("fp6_lora", _TYPE[X.dtype], call.ptr(X, X.dtype, "X"), M, a, b, L, rank, call.optional(index, torch.int32, "index", (M,)),
+                call.optional(scaling, torch.float32, "scaling", (L,)), call.ptr(Y, X.dtype, "Y", (M, N)), N, K,
+                call.ptr(out, X.dtype, "out", (M, N)), call.optional(hidden, torch.float32, "hidden", (M, rank)), ws, wb)
+    return out
+
+
+def fp6_lora_group_workspace_bytes(M: int, shapes, adapters: int = 1) -> int:
+    """Workspace for projections given as (N, K, rank) triples."""
+    arr = (LoraProblem * len(shapes))()
+    for i, (N, K, rank) in enumerate(shapes):
+        arr[i] = LoraProblem(None, None, None, None, None, None, N, K, rank)
+    return int(lib().fp6_lora_group_workspace_bytes(M, arr, len(shapes), adapters))
+
+
+def fp6_lora_group(layers, index: Optional[torch.Tensor] = None, scaling: Optional[torch.Tensor] = None, outs=None,
+                   workspace: Optional[torch.Tensor] = None):
+    """fp6_lora for up to FP6_GROUP_MAX projections [(X, A, B, Y), ...] of the same rows, whose adapters and scaling are common, in
+    one call.  Returns the list of results (without `outs`: the Y themselves)."""
+    if not 1 <= len(layers) <= FP6_GROUP_MAX:
+        raise Fp6Error("a group holds 1 to %d projections" % FP6_GROUP_MAX)
+    if outs is not None and len(outs) != len(layers):
+        raise Fp6Error("outs must hold one tensor per projection")
+    call = _Call(layers[0][0], "X")
+    arr = (LoraProblem * len(layers))()
+    results, shapes, first = [], [], layers[0][0]
+    for i, (X, A, B, Y) in enumerate(layers):
+        a, b, L, rank, N, K = _adapters(call, X, A, B)
+        if X.dtype != first.dtype or X.shape[0] != first.shape[0] or L != layers[0][1].shape[0]:
+            raise Fp6Error("the projections of a group share type, rows and adapters")
+        out = Y if outs is None or outs[i] is None else outs[i]
+        arr[i] = LoraProblem(call.ptr(X, X.dtype, "X"), a, b, call.ptr(Y, X.dtype, "Y", (X.shape[0], N)),
+                             call.ptr(out, X.dtype, "out", (X.shape[0], N)), None, N, K, rank)
+        results.append(out)
+        shapes.append((N, K, rank))
+    M = first.shape[0]
+    ws, wb, workspace = call.workspace(workspace, lambda: fp6_lora_group_workspace_bytes(M, shapes, L))
+    call.launch("fp6_lora_group", _TYPE[first.dtype], M, arr, len(layers), L, call.optional(index, torch.int32, "index", (M,)),
+                call.optional(scaling, torch.float32, "scaling", (L,)), ws, wb)
+    return results
+
+
+def fp6_lora_backward_workspace_bytes(M: int, N: int, K: int, rank: int, adapters: int = 1) -> int:
+    return int(lib().fp6_lora_backward_workspace_bytes(M, N, K, rank, adapters))
+
+
+def fp6_lora_backward(dY: torch.Tensor, X: torch.Tensor, hidden: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                      dX: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None, scaling: Optional[torch.Tensor] = None,
+                      dA: Optional[torch.Tensor] = None, dB: Optional[torch.Tensor] = None, accumulate: bool = False,
+                      out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """The gradients of fp6_lora: (dX + scaling dY B A, dA, dB); dX None: no gradient for X.  dA and dB are fp32 and are added to
+    where `accumulate` is set; `out` may be dX and is dX where it is not given."""
+    call = _Call(X, "X")
+    a, b, L, rank, N, K = _adapters(call, X, A, B)
+    M = X.shape[0]
+    if accumulate and (dA is None or dB is None):
+        raise Fp6Error("accumulate needs dA and dB")
+    if out is not None and dX is None:
+        raise Fp6Error("out needs dX")
+    out = dX if out is None else out
+    if dA is None:
+        dA = torch.empty((L, rank, K), dtype=torch.float32, device=X.device)
+    if dB is None:
+        dB = torch.empty((L, N, rank), dtype=torch.float32, device=X.device)
+    ws, wb, workspace = call.workspace(workspace, lambda: fp6_lora_backward_workspace_bytes(M, N, K, rank, L))
+    call.launch("fp6_lora_backward", _TYPE[X.dtype], call.ptr(dY, X.dtype, "dY", (M, N)), call.ptr(X, X.dtype, "X"),
+                call.ptr(hidden, torch.float32, "hidden", (M, rank)), M, a, b, L, rank, call.optional(index, torch.int32, "index", (M,)),
+                call.optional(scaling, torch.float32, "scaling", (L,)), call.optional(dX, X.dtype, "dX", (M, K)),
+                call.optional(out, X.dtype, "out", (M, K)), call.ptr(dA, torch.float32, "dA", (L, rank, K)),
+                call.ptr(dB, torch.float32, "dB", (L, N, rank)), int(bool(accumulate)), N, K, ws, wb)
+    return out, dA, dB
+
+
+def fp6_transpose_pack(hi: torch.Tensor, lo: torch.Tensor, scales: torch.Tensor, N: int, K: int, format: int = FP6_FORMAT_E3M2):
+    """Planes and row scales of [N,K] -> (hi_t, lo_t, scales_t fp16 [K], ratio fp32 [N]): the weight packed turned, for fp6_linear_grad."""
+    call = _Call(hi, "hi_plane")
+    _shape_ok(N, K)
+    div = 8 if format == FP6_FORMAT_E3M1 else 4
+    h, l = call.flat(hi, torch.uint8, "hi_plane", N * K // 2), call.flat(lo, torch.uint8, "lo_plane", N * K // div)
+    s = call.flat(scales, torch.float16, "scales", N)
+    hi_t, lo_t = torch.empty_like(hi), torch.empty_like(lo)
+    scales_t = torch.empty((K,), dtype=torch.float16, device=hi.device)
+    ratio = torch.empty((N,), dtype=torch.float32, device=hi.device)
+    call.launch("fp6_transpose_pack", format, h, l, s, N, K, hi_t.data_ptr(), lo_t.data_ptr(), scales_t.data_ptr(), ratio.data_ptr())
+    return hi_t, lo_t, scales_t, ratio
+
+
+def fp6_linear_grad_workspace_bytes(M: int, N: int, K: int, format: int = FP6_FORMAT_E3M2) -> int:
+    return int(lib().fp6_linear_grad_workspace_bytes(format, M, N, K))
+
+
+def fp6_linear_grad(dY: torch.Tensor, hi_t: torch.Tensor, lo_t: torch.Tensor, scales_t: torch.Tensor, ratio: torch.Tensor, N: int, K: int,
+                    format: int = FP6_FORMAT_E3M2, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dX[M,K] = dY[M,N] x dequant(planes): the gradient of the frozen layer by its input, from the planes of fp6_transpose_pack."""
+    call = _Call(dY, "dY")
+    _shape_ok(N, K)
+    dtype = torch.bfloat16 if format == FP6_FORMAT_E3M2_V2_BF16 else torch.float16
+    if dY.dim() != 2 or dY.shape[1] != N or dY.shape[0] < 1:
+        raise Fp6Error("dY must be [M,N] with M >= 1")
+    M, div = dY.shape[0], 8 if format == FP6_FORMAT_E3M1 else 4
+    if out is None:
+        out = torch.empty((M, K), dtype=dtype, device=dY.device)
+    ws, wb, workspace = call.workspace(workspace, lambda: fp6_linear_grad_workspace_bytes(M, N, K, format))
+    call.launch("fp6_linear_grad", format, call.ptr(dY, dtype, "dY"), M, call.flat(hi_t, torch.uint8, "hi_t", N * K // 2),
+                call.flat(lo_t, torch.uint8, "lo_t", N * K // div), call.flat(scales_t, torch.float16, "scales_t", K),
+                call.flat(ratio, torch.float32, "ratio", N), N, K, call.ptr(out, dtype, "dX", (M, K)), ws, wb)
+    return out
+
+
+class AdamWPlan:
+    """The tensors of an optimiser step, checked once, and their table in device memory; keeps the tensors alive."""
+
+    def __init__(self, table: torch.Tensor, items: int, state_bits: int, grad_type: int, copy_type: int, tensors):
+        self.table, self.items, self.state_bits, self.grad_type, self.copy_type = table, items, state_bits, grad_type, copy_type
+        self.tensors = tensors
+
+
+def fp6_adamw_plan(params, grads, first, second, first_scales=None, second_scales=None, copies=None) -> AdamWPlan:
+    """Plan of an AdamW step: lists of equally many tensors.  params fp32; grads all fp32, all fp16 or all bf16; first and second
+    fp32 (m and v), or torch.float8_e4m3fn (m and sqrt(v), with uint8 scales, one per 256 elements); copies fp16 or bf16, or None."""
+    lists = [list(x) if x is not None else None for x in (params, grads, first, second, first_scales, second_scales, copies)]
+    n = len(lists[0])
+    if n < 1 or any(x is not None and len(x) != n for x in lists):
+        raise Fp6Error("a plan takes lists of equally many tensors, one at least")
+    if not all(isinstance(t, torch.Tensor) for x in lists if x is not None for t in x):
+        raise Fp6Error("a plan takes lists of tensors")
+    params, grads, first, second, first_scales, second_scales, copies = lists
+    eight = first[0].dtype == torch.float8_e4m3fn
+    if eight != (first_scales is not None) or eight != (second_scales is not None):
+        raise Fp6Error("states in 8 bits come with scales, states in 32 without")
+    state = torch.float8_e4m3fn if eight else torch.float32
+    if grads[0].dtype not in _TYPE or (copies is not None and copies[0].dtype not in (torch.float16, torch.bfloat16)):
+        raise Fp6Error("grads must be fp32, fp16 or bf16, copies fp16 or bf16")
+    call = _Call(params[0], "param")
+    arr = (AdamWTensor * n)()
+    for i in range(n):
+        p, count = params[i], params[i].numel()
+
+        def like(t, dtype, what):
+            ptr = call.ptr(t, dtype, what)
+            if t.numel() != count:
+                raise Fp6Error("%s %d holds %d elements, its param %d" % (what, i, t.numel(), count))
+            return ptr
+
+        blocks = (-(-count // 256),)
+        arr[i] = AdamWTensor(call.ptr(p, torch.float32, "param"), like(grads[i], grads[0].dtype, "grad"), like(first[i], state, "first"),
+                             like(second[i], state, "second"),
+                             call.ptr(first_scales[i], torch.uint8, "first_scales", blocks) if eight else None,
+                             call.ptr(second_scales[i], torch.uint8, "second_scales", blocks) if eight else None,
+                             like(copies[i], copies[0].dtype, "copy") if copies is not None else None, count)
+    bits, grad_type = 8 if eight else 32, _TYPE[grads[0].dtype]
+    copy_type = FP6_NO_COPY if copies is None else _TYPE[copies[0].dtype]
+    host = torch.zeros(int(lib().fp6_adamw_plan_bytes(arr, n)), dtype=torch.uint8)
+    items = ctypes.c_int64()
+    _check(lib().fp6_adamw_plan(arr, n, bits, grad_type, copy_type, host.data_ptr(), host.numel(), ctypes.byref(items)), "fp6_adamw_plan")
+    return AdamWPlan(host.to(call.device), items.value, bits, grad_type, copy_type, lists)
+
+
+def fp6_adamw(plan: AdamWPlan, step: torch.Tensor, lr=1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+              weight_decay: float = 0.01, grad_scale: Optional[torch.Tensor] = None, found_inf: Optional[torch.Tensor] = None,
+              seed: int = 0) -> None:
+    """One AdamW step over the tensors of the plan, in place.  step: int32 [1], the steps done so far, counted on by the call; lr: a
+    number, or fp32 [1] on the device; grad_scale fp32 [1] multiplies the gradients; found_inf fp32 [1]: not 0, and nothing changes."""
+    call = _Call(plan.table, "plan")
+    on_device = isinstance(lr, torch.Tensor)
+    options = AdamWOptions(0.0 if on_device else float(lr), beta1, beta2, eps, weight_decay,
+                           call.ptr(lr, torch.float32, "lr", (1,)) if on_device else None,
+                           call.optional(grad_scale, torch.float32, "grad_scale", (1,)),
+                           call.optional(found_inf, torch.float32, "found_inf", (1,)), int(seed) & 0xFFFFFFFF)
+    call.launch("fp6_adamw", plan.table.data_ptr(), plan.items, plan.state_bits, plan.grad_type, plan.copy_type,
+                call.ptr(step, torch.int32, "step", (1,)), ctypes.byref(options))
 
 
 # ---- measurement probes (kernels that only read, or only issue MFMAs)

@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfp6_linear.so")
 SOURCES = ["fp6_abi.hip", "fp6_pack.hip", "fp6_decode.hip", "fp6_gemm.hip", "fp6_gemm_variants.hip", "fp6_gemm_bf16.hip",
-           "fp6_gemm_heights.hip", "fp6_gemm_heights_v2.hip", "fp6_gemm_heights_fp5_fgq.hip", "fp6_probes.hip"]
+           "fp6_gemm_heights.hip", "fp6_gemm_heights_v2.hip", "fp6_gemm_heights_fp5_fgq.hip", "fp6_probes.hip",
+           "fp6_adapters_abi.hip", "fp6_lora.hip", "fp6_grad.hip", "fp6_adamw.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
          # packed-fp32 VALU forms are switched off for every kernel of this library
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -627,6 +627,8 @@ const char* fp6_status_string(int status)
         case FP6_ERR_VARIANT: return "kernel variant or split_k not valid for this shape";
         case FP6_ERR_HIP: return "HIP launch error";
         case FP6_ERR_SCRATCH: return "this shape needs more than the FP6_STATIC_SCRATCH_BYTES of built-in scratch: use fp6_linear with a workspace";
+        case FP6_ERR_OVERLAP: return "a buffer that is written overlaps another one";
+        case FP6_ERR_VALUE: return "a type, rank, count or other number is outside what the call takes";
         default: return "unknown status";
     }
 }

@@ -101,4 +101,28 @@ hipError_t launch_gemm(const LinearPlan& p, const uint16_t* X, int64_t M, const 
                        const uint16_t* scales, int64_t N, int64_t K, uint16_t* Y, void* workspace,
                        hipStream_t stream);
 
+// fp6_lora.hip
+struct LoraBackward {
+    const uint16_t *dY, *X;
+    const float* hidden;
+    const uint16_t *A, *B;
+    const int32_t* index;
+    const float* scaling;
+    const uint16_t* dX;
+    uint16_t* out;          // NULL: no gradient by X
+    float *dA, *dB;
+    int64_t M, N, K;
+    int rank, adapters, accumulate;
+};
+size_t lora_workspace(int64_t M, const fp6_lora_problem* problems, int count, int adapters);
+hipError_t launch_lora(bool bf16, int64_t M, const fp6_lora_problem* problems, int count, int adapters, const int32_t* index,
+                       const float* scaling, void* workspace, hipStream_t stream);
+size_t lora_backward_workspace(int64_t M, int64_t N, int64_t K, int rank, int adapters);
+hipError_t launch_lora_backward(bool bf16, const LoraBackward& b, void* workspace, hipStream_t stream);
+
+// fp6_grad.hip
+hipError_t launch_transpose_pack(int format, const void* hi, const void* lo, const uint16_t* scales, int64_t N, int64_t K, void* hi_t,
+                                 void* lo_t, uint16_t* scales_t, float* ratio, hipStream_t stream);
+hipError_t launch_scale_rows(bool bf16, const uint16_t* dY, const float* ratio, int64_t M, int64_t N, uint16_t* out, hipStream_t stream);
+
 }  // namespace fp6
