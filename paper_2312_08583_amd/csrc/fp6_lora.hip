@@ -63,6 +63,20 @@ __device__ __forceinline__ void split_terms(float v, uint16_t (&t)[TERMS])
     }
 }
 
+// A load whose lanes hold a 4 x 16 block of 16-bit numbers row by row, four a lane, and get back its columns.
+__device__ __forceinline__ u32x2 read_turned(const uint16_t* p)
+{
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p));
+}
+
+// Accesses of a wavefront to LDS of its own are carried out in order; the compiler has to keep them so.
+__device__ __forceinline__ void own_lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // ------------------------------------------------------------------ shrink
 struct ShrinkLayer {
     const uint16_t* Q;      // [M, C]
@@ -81,30 +95,32 @@ struct ShrinkArgs {
     int adapters, slots;
 };
 
+template <int JT, int RT, bool TURNED>
+constexpr int kShrinkLds = TURNED && 4 * 64 * (16 * JT + 8) * 2 > 4 * RT * JT * 1024 ? 4 * 64 * (16 * JT + 8) * 2 : 4 * RT * JT * 1024;
+
 // P[slice][m][j] = sum over the slice's c of Q[m][c] W[a][j][c].  A workgroup: 16 * RT rows, one slice of the contraction, whose
 // 64-wide units its four wavefronts take in turn; a lane holds 16 consecutive values of a row per unit (whole lines).  The
 // distinct adapters of the rows are taken one after another, or one per grid slot: each reads its own A.
 template <int FMT, int JT, int RT, bool TURNED>
-__global__ __launch_bounds__(256) void lora_shrink_kernel(ShrinkArgs args)
+__device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, int slot, unsigned char* shared)
 {
     constexpr int kLd = 16 * JT + 8;                       // turned: elements between two rows of the staged unit
-    __shared__ __align__(16) unsigned char shared[TURNED && 4 * 64 * kLd * 2 > 4 * RT * JT * 1024 ? 4 * 64 * kLd * 2 : 4 * RT * JT * 1024];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
     int which = 0;
-    while (which + 1 < args.layers && (int)blockIdx.x >= args.layer[which + 1].first) which++;
+    while (which + 1 < args.layers && block >= args.layer[which + 1].first) which++;
     const ShrinkLayer L = args.layer[which];
-    const int at = (int)blockIdx.x - L.first, slice = at % L.slices;
+    const int at = block - L.first, slice = at % L.slices;
     const int64_t m0 = (int64_t)(at / L.slices) * (16 * RT);
     const int rank = L.rank, C = L.C, units = C / 64;
     const int u_begin = slice_begin(units, L.slices, slice) + wave, u_end = slice_begin(units, L.slices, slice + 1);
 
-    // (16 * RT <= 32 rows: lane l looks after row l)
+    // (16 * RT <= 64 rows: lane l looks after row l)
     const int mine = lane < 16 * RT ? adapter_of(args.index, m0 + lane, args.M, args.adapters) : kNoAdapter;
     uint64_t pending = __ballot(mine != kNoAdapter);
-    const uint64_t none = ~pending & (((uint64_t)1 << (16 * RT)) - 1);
+    const uint64_t none = RT == 4 ? ~pending : ~pending & (((uint64_t)1 << (16 * (RT & 3))) - 1);
     float* P = L.P + (size_t)slice * args.M * rank;
-    if (blockIdx.y == 0 && none) {                         // rows without an adapter
+    if (slot == 0 && none) {                               // rows without an adapter
         for (int e = threadIdx.x; e < 16 * RT * rank; e += 256)
             if ((none >> (e / rank)) & 1 && m0 + e / rank < args.M) P[(size_t)(m0 + e / rank) * rank + e % rank] = 0.0f;
     }
@@ -114,62 +130,88 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(ShrinkArgs args)
         const int64_t row = min(m0 + 16 * t + i, args.M - 1);
         q[t] = L.Q + (size_t)row * C + 16 * g;
     }
+    // turned: the unit's 64 rows of W are one piece of memory, 2 * JT times 16 bytes a lane at most; where each goes in LDS
+    uint16_t* own = reinterpret_cast<uint16_t*>(shared) + wave * (64 * kLd);
+    const int per_row = rank / 8;
+    int put[2 * JT];
+    if (TURNED) {
+#pragma unroll
+        for (int k = 0; k < 2 * JT; k++) {
+            const int p = lane + 64 * k;
+            put[k] = (p / per_row) * kLd + (p % per_row) * 8;
+        }
+    }
     for (int seen = 0; pending; seen++) {
         const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(pending));
         const uint64_t rows = __ballot(mine == a);
         pending &= ~rows;
-        if (seen % args.slots != (int)blockIdx.y) continue;
+        if (seen % args.slots != slot) continue;
         const uint16_t* W = L.W + (size_t)a * rank * C;
+        const uint16_t* wj[JT];
+#pragma unroll
+        for (int j = 0; j < JT; j++) wj[j] = W + (size_t)min(16 * j + i, rank - 1) * C + 16 * g;
         float4v acc[RT][JT];
 #pragma unroll
         for (int t = 0; t < RT; t++)
 #pragma unroll
             for (int j = 0; j < JT; j++) acc[t][j] = float4v{0, 0, 0, 0};
-        for (int u = u_begin; u < u_end; u += 4) {
-            u32x4 x[RT][2], w[JT][2];
+        struct Unit {
+            u32x4 x[RT][2], w[JT][2];          // (turned: w is the piece as it lies in memory)
+        };
+        auto load = [&](Unit& b, int u) {
 #pragma unroll
             for (int t = 0; t < RT; t++)
 #pragma unroll
-                for (int h = 0; h < 2; h++) x[t][h] = *reinterpret_cast<const u32x4*>(q[t] + (size_t)u * 64 + 8 * h);
+                for (int h = 0; h < 2; h++) b.x[t][h] = *reinterpret_cast<const u32x4*>(q[t] + (size_t)u * 64 + 8 * h);
             if (!TURNED) {
 #pragma unroll
                 for (int j = 0; j < JT; j++)
 #pragma unroll
-                    for (int h = 0; h < 2; h++)
-                        w[j][h] = *reinterpret_cast<const u32x4*>(W + (size_t)min(16 * j + i, rank - 1) * C + (size_t)u * 64 + 16 * g + 8 * h);
+                    for (int h = 0; h < 2; h++) b.w[j][h] = *reinterpret_cast<const u32x4*>(wj[j] + (size_t)u * 64 + 8 * h);
             } else {
-                // the unit's 64 rows of W (one piece of memory) through the wavefront's own LDS, read back turned
-                unsigned char* own = shared + wave * (64 * kLd * 2);
                 const u32x4* piece = reinterpret_cast<const u32x4*>(W + (size_t)u * 64 * rank);
-                const int per_row = rank / 8;
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                for (int p = lane; p < 64 * per_row; p += 64)
-                    *reinterpret_cast<u32x4*>(own + ((p / per_row) * kLd + (p % per_row) * 8) * 2) = piece[p];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int j = 0; j < JT; j++)
+                for (int k = 0; k < 2 * JT; k++) b.w[k >> 1][k & 1] = piece[min(lane + 64 * k, 64 * per_row - 1)];
+            }
+        };
+        auto compute = [&](const Unit& b) {
+            if (TURNED) {
+                own_lds_order();
 #pragma unroll
-                    for (int h = 0; h < 2; h++)
-#pragma unroll
-                        for (int e = 0; e < 2; e++) {
-                            typedef short s4 __attribute__((ext_vector_type(4)));
-                            const int row = 16 * g + 8 * h + 4 * e + (i >> 2), col = min(16 * j + 4 * (i & 3), rank - 4);
-                            const s4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (__attribute__((address_space(3))) s4*)(own + (row * kLd + col) * 2));
-                            const u32x2 d = __builtin_bit_cast(u32x2, r);
-                            w[j][h][2 * e] = d[0];
-                            w[j][h][2 * e + 1] = d[1];
-                        }
+                for (int k = 0; k < 2 * JT; k++)
+                    if (lane + 64 * k < 64 * per_row) *reinterpret_cast<u32x4*>(own + put[k]) = b.w[k >> 1][k & 1];
+                own_lds_order();
             }
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
-                for (int t = 0; t < RT; t++)
+                for (int j = 0; j < JT; j++) {
+                    u32x4 w = b.w[j][h];
+                    if (TURNED) {
 #pragma unroll
-                    for (int j = 0; j < JT; j++)
-                        acc[t][j] = mfma16x16x32_of<FMT>(__builtin_bit_cast(half8, x[t][h]), __builtin_bit_cast(half8, w[j][h]), acc[t][j]);
+                        for (int e = 0; e < 2; e++) {
+                            const u32x2 d = read_turned(own + (16 * g + 8 * h + 4 * e + (i >> 2)) * kLd + min(16 * j + 4 * (i & 3), rank - 4));
+                            w[2 * e] = d[0];
+                            w[2 * e + 1] = d[1];
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < RT; t++)
+                        acc[t][j] = mfma16x16x32_of<FMT>(__builtin_bit_cast(half8, b.x[t][h]), __builtin_bit_cast(half8, w), acc[t][j]);
+                }
+        };
+        if (u_begin < u_end) {
+            // one unit in flight while another is used (past the end: the last one again, so that the loads need no branch)
+            Unit b[2];
+            const int last = u_begin + (u_end - 1 - u_begin) / 4 * 4;
+            load(b[0], u_begin);
+            for (int u = u_begin; u < u_end; u += 8) {
+                if (RT > 1 || u + 4 < u_end) load(b[1], min(u + 4, last));
+                compute(b[0]);
+                if (u + 4 >= u_end) break;
+                if (RT > 1 || u + 8 < u_end) load(b[0], min(u + 8, last));
+                compute(b[1]);
+            }
         }
         // the four wavefronts' sums meet in LDS, added in their order
         __syncthreads();
@@ -195,13 +237,66 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(ShrinkArgs args)
     }
 }
 
+template <int FMT, int JT, int RT, bool TURNED>
+__global__ __launch_bounds__(256) void lora_shrink_kernel(ShrinkArgs args)
+{
+    __shared__ __align__(16) unsigned char shared[kShrinkLds<JT, RT, TURNED>];
+    shrink_block<FMT, JT, RT, TURNED>(args, blockIdx.x, blockIdx.y, shared);
+}
+
+// ------------------------------------------------------------------ finish
+struct FinishArgs {
+    const float* P;          // [slices, M, rank]
+    float* sum;              // [M, rank]: the slices added up (NULL: not wanted; may be P)
+    uint16_t* terms;         // [M][2][rank]: the sum as two 16-bit terms of a row times 2^exponent
+    float* power;            // [M]: 2^exponent
+    int64_t M;
+    int rank, slices, lanes; // lanes that share a row (a power of two, at least rank / 4)
+};
+
+// The slices of the contraction added up, in their order, and split into the two terms that the expand kernel multiplies with: once a row
+// instead of once a row and block of columns.
+template <int FMT>
+__global__ __launch_bounds__(256) void lora_finish_kernel(FinishArgs args)
+{
+    const int lanes = args.lanes, rank = args.rank;
+    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
+    const int j = 4 * (int)(threadIdx.x % lanes);
+    const bool real = row < args.M && j < rank;
+    float4v v = float4v{0, 0, 0, 0};
+    if (real) {
+        const float* p = args.P + (size_t)row * rank + j;
+        const size_t step = (size_t)args.M * rank;
+#pragma unroll 8
+        for (int c = 0; c < args.slices; c++) v += *reinterpret_cast<const float4v*>(p + c * step);
+        if (args.sum) *reinterpret_cast<float4v*>(args.sum + (size_t)row * rank + j) = v;
+    }
+    int exponent = 0;
+    if (FMT != kE3M2B) {
+        float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+        for (int off = 1; off < lanes; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+        exponent = exponent_for(top);
+        v *= power_of_two(-exponent);
+    }
+    if (!real) return;
+    uint16_t t[4][2];
+#pragma unroll
+    for (int e = 0; e < 4; e++) split_terms<FMT>(v[e], t[e]);
+    uint16_t* to = args.terms + (size_t)row * 2 * rank + j;
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+        *reinterpret_cast<u32x2*>(to + k * rank) = u32x2{t[0][k] | (uint32_t)t[1][k] << 16, t[2][k] | (uint32_t)t[3][k] << 16};
+    if (j == 0) args.power[row] = power_of_two(exponent);
+}
+
 // ------------------------------------------------------------------ expand
 struct ExpandLayer {
-    const float* P;         // [slices, M, rank]
+    const float* P;         // SLICED: [slices, M, rank]; else the power of two of each row
+    const uint16_t* terms;  // else: [M][2][rank]
     const uint16_t* W;      // [adapters, D, rank], turned: [adapters, rank, D]
     const uint16_t* Y;      // [M, D]
     uint16_t* out;          // [M, D] (may be Y)
-    float* hidden;          // [M, rank]: the sum of the slices is kept here (NULL: it is not)
+    float* hidden;          // SLICED: [M, rank]: the sum of the slices is kept here (NULL: it is not)
     int D, rank, slices;
     int first;
 };
@@ -215,148 +310,240 @@ struct ExpandArgs {
     int adapters, slots, row_tiles;      // row tiles of 16 rows per workgroup
 };
 
-// out[m][n] = Y[m][n] + s * sum_j P[m][j] W[n][j].  A wavefront: 64 columns n, 16 rows at a time; the lane of row l % 16 holds 16
-// consecutive columns (the rows of the W operand are dealt out so that it does).  P is split into two 16-bit terms; with fp16 each
-// row has a power of two that brings it into range.  PACKED (rank <= 16): both terms share one MFMA of contraction 32.
-template <int FMT, int JS, bool PACKED, bool TURNED>
-__global__ __launch_bounds__(256) void lora_expand_kernel(ExpandArgs args)
+constexpr int kExpandLd = 64 + 8;        // turned: elements between two rows of a staged piece of W
+template <bool TURNED>
+constexpr int kExpandLds = TURNED ? 4 * 32 * kExpandLd * 2 : 16;
+
+// out[m][n] = Y[m][n] + s * sum_j P[m][j] W[n][j].  A wavefront: 64 * CB columns n, 16 rows at a time; the lane of row l % 16 holds two
+// pieces of eight consecutive columns of each 64 (the rows of the W operand are dealt out so that it does).  P is two 16-bit terms
+// times a power of two per row.  PACKED (rank <= 16): both terms share one MFMA of contraction 32.  W stays in registers from row
+// tile to row tile as long as the adapter is the same.  SLICED (few rows): the terms are made here from the slices.
+template <int FMT, int JS, bool PACKED, bool TURNED, bool SLICED, int CB>
+__device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, int slot, unsigned char* shared)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
     int which = 0;
-    while (which + 1 < args.layers && (int)blockIdx.x >= args.layer[which + 1].first) which++;
+    while (which + 1 < args.layers && block >= args.layer[which + 1].first) which++;
     const ExpandLayer L = args.layer[which];
-    const int blocks = (L.D / 64 + 3) / 4, at = (int)blockIdx.x - L.first;
-    const int n0 = ((at % blocks) * 4 + wave) * 64, rank = L.rank, D = L.D;
+    const int rank = L.rank, D = L.D, per_block = 256 * CB, blocks = (D + per_block - 1) / per_block, at = block - L.first;
+    const int n0 = (at % blocks) * per_block + wave * (64 * CB);
     if (n0 >= D) return;
     const int64_t tile0 = (int64_t)(at / blocks) * args.row_tiles;
+    const int64_t tiles = min((int64_t)args.row_tiles, (args.M + 15) / 16 - tile0);
+    constexpr int TERMS = PACKED ? 1 : 2;
+
+    struct Rows {                        // what a row tile needs: Y, the owner, and P where it is ready
+        u32x4 y[CB][2], p[JS][TERMS];
+        float power;
+        int mine;
+    };
+    auto load = [&](Rows& b, int64_t t) {
+        const int64_t row = (tile0 + t) * 16 + i;
+        b.mine = adapter_of(args.index, row, args.M, args.adapters);
+        const int64_t near = min(row, args.M - 1);
+        const uint16_t* y = L.Y + (size_t)near * D + n0 + 8 * g;
+#pragma unroll
+        for (int c = 0; c < CB; c++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int off = 64 * c + 32 * h;
+                b.y[c][h] = *reinterpret_cast<const u32x4*>(y + (n0 + off < D ? off : 0));
+            }
+        if (!SLICED) {
+            const uint16_t* p = L.terms + (size_t)near * 2 * rank;
+            b.power = FMT != kE3M2B ? L.P[near] : 1.0f;
+#pragma unroll
+            for (int s = 0; s < JS; s++)
+#pragma unroll
+                for (int k = 0; k < TERMS; k++) {
+                    const int j0 = 32 * s + 8 * g, most = PACKED ? 2 * rank : rank;
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(p + k * rank + min(j0, most - 8));
+                    b.p[s][k] = j0 < most ? v : u32x4{0, 0, 0, 0};
+                }
+        }
+    };
 
     int held = kNoAdapter;               // the adapter whose operands are in w
-    half8 w[4][JS];
-    for (int t = 0; t < args.row_tiles; t++) {
-        const int64_t m0 = (tile0 + t) * 16, row = m0 + i;
-        if (m0 >= args.M) break;
-        const int mine = adapter_of(args.index, row, args.M, args.adapters);
-        uint64_t pending = __ballot(mine != kNoAdapter) & 0xFFFF;
-        const size_t where = (size_t)row * D + n0 + 16 * g;
-        if (mine == kNoAdapter && blockIdx.y == 0 && row < args.M) {
-            if (L.out != L.Y) {
-                const u32x4* from = reinterpret_cast<const u32x4*>(L.Y + where);
-                u32x4* to = reinterpret_cast<u32x4*>(L.out + where);
-                const u32x4 a = from[0], b = from[1];
-                to[0] = a;
-                to[1] = b;
-            }
-            if (L.hidden && n0 == 0)
-                for (int j = 4 * g; j < rank; j += 16) *reinterpret_cast<float4v*>(L.hidden + (size_t)row * rank + j) = float4v{0, 0, 0, 0};
-        }
-        for (int seen = 0; pending; seen++) {
-            const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(pending));
-            pending &= ~(__ballot(mine == a) & 0xFFFF);
-            if (seen % args.slots != (int)blockIdx.y) continue;
-            // P of this lane's row: eight values per step
-            float v[JS][8];
-            float top = 0.0f;
+    u32x4 w[CB][4][JS];
+    auto hold = [&](int a) {
+        held = a;
+        const uint16_t* W = L.W + (size_t)a * rank * D;
 #pragma unroll
-            for (int s = 0; s < JS; s++) {
-                const int k0 = 32 * s + 8 * g, j0 = PACKED && k0 >= rank ? k0 - rank : k0;
+        for (int s = 0; s < JS; s++) {
+            const int k0 = 32 * s + 8 * g, j0 = PACKED && k0 >= rank ? k0 - rank : k0;
 #pragma unroll
-                for (int e = 0; e < 8; e++) v[s][e] = 0.0f;
-                if (mine == a && j0 < rank) {
-                    for (int c = 0; c < L.slices; c++) {
-                        const float4v* p = reinterpret_cast<const float4v*>(L.P + ((size_t)c * args.M + row) * rank + j0);
-                        const float4v lo = p[0], hi = p[1];
+            for (int c = 0; c < CB; c++) {
+                const int nc = n0 + 64 * c < D ? n0 + 64 * c : n0;          // (past the end: columns that are not stored)
+                if (!TURNED) {
 #pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            v[s][e] += lo[e];
-                            v[s][4 + e] += hi[e];
-                        }
+                    for (int t = 0; t < 4; t++) {
+                        const int n = nc + 32 * (t >> 1) + 8 * (i >> 2) + 4 * (t & 1) + (i & 3);
+                        const u32x4 d = *reinterpret_cast<const u32x4*>(W + (size_t)n * rank + min(j0, rank - 8));
+                        w[c][t][s] = j0 < rank ? d : u32x4{0, 0, 0, 0};
                     }
-                    if (L.hidden && n0 == 0 && j0 == k0) {
-                        float4v* h = reinterpret_cast<float4v*>(L.hidden + (size_t)row * rank + j0);
-                        h[0] = float4v{v[s][0], v[s][1], v[s][2], v[s][3]};
-                        h[1] = float4v{v[s][4], v[s][5], v[s][6], v[s][7]};
+                } else {
+                    // 32 rows j of 64 columns through the wavefront's own LDS
+                    uint16_t* own = reinterpret_cast<uint16_t*>(shared) + wave * (32 * kExpandLd);
+                    u32x4 d[4];
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        const int j = 32 * s + (lane >> 3) + 8 * k;
+                        d[k] = *reinterpret_cast<const u32x4*>(W + (size_t)min(j, rank - 1) * D + nc + 8 * (lane & 7));
+                    }
+                    own_lds_order();
+#pragma unroll
+                    for (int k = 0; k < 4; k++) *reinterpret_cast<u32x4*>(own + ((lane >> 3) + 8 * k) * kExpandLd + 8 * (lane & 7)) = d[k];
+                    own_lds_order();
+                    const int row = PACKED ? min(j0, rank - 8) : 8 * g;
+#pragma unroll
+                    for (int t = 0; t < 4; t++) {
+                        u32x4 x;
+#pragma unroll
+                        for (int e = 0; e < 2; e++) {
+                            const u32x2 r = read_turned(own + (row + 4 * e + (i >> 2)) * kExpandLd + 32 * (t >> 1) + 8 * (i & 3) + 4 * (t & 1));
+                            x[2 * e] = r[0];
+                            x[2 * e + 1] = r[1];
+                        }
+                        w[c][t][s] = j0 < rank ? x : u32x4{0, 0, 0, 0};
                     }
                 }
-#pragma unroll
-                for (int e = 0; e < 8; e++) top = fmaxf(top, fabsf(v[s][e]));
             }
-            int exponent = 0;
-            if (FMT != kE3M2B) {
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                exponent = exponent_for(top);
-                const float down = power_of_two(-exponent);
-#pragma unroll
-                for (int s = 0; s < JS; s++)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) v[s][e] *= down;
-            }
-            if (a != held) {
-                held = a;
-                const uint16_t* W = L.W + (size_t)a * rank * D;
+        }
+    };
+
+    auto work = [&](Rows& b, int64_t t) {
+        const int64_t row = (tile0 + t) * 16 + i;
+        uint64_t pending = __ballot(b.mine != kNoAdapter) & 0xFFFF;
+        bool store = b.mine == kNoAdapter && slot == 0 && row < args.M && L.out != L.Y;
+        if (SLICED && L.hidden && n0 == 0 && slot == 0 && b.mine == kNoAdapter && row < args.M)
+            for (int j = 4 * g; j < rank; j += 16) *reinterpret_cast<float4v*>(L.hidden + (size_t)row * rank + j) = float4v{0, 0, 0, 0};
+        for (int seen = 0; pending; seen++) {
+            const int a = __builtin_amdgcn_readlane(b.mine, __builtin_ctzll(pending));
+            pending &= ~(__ballot(b.mine == a) & 0xFFFF);
+            if (seen % args.slots != slot) continue;
+            if (a != held) hold(a);
+            if (SLICED) {
+                // P of this lane's row: eight values per step
+                float v[JS][8];
+                float top = 0.0f;
 #pragma unroll
                 for (int s = 0; s < JS; s++) {
                     const int k0 = 32 * s + 8 * g, j0 = PACKED && k0 >= rank ? k0 - rank : k0;
-#pragma unroll
-                    for (int c = 0; c < 4; c++) {
-                        const int n = n0 + 16 * (i >> 2) + 4 * c + (i & 3);
-                        u32x4 d = u32x4{0, 0, 0, 0};
-                        if (j0 < rank) {
-                            if (!TURNED) {
-                                d = *reinterpret_cast<const u32x4*>(W + (size_t)n * rank + j0);
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 4; e++)
-                                    d[e] = (uint32_t)W[(size_t)(j0 + 2 * e) * D + n] | (uint32_t)W[(size_t)(j0 + 2 * e + 1) * D + n] << 16;
-                            }
+                    float4v lo = float4v{0, 0, 0, 0}, hi = lo;
+                    if (b.mine == a && j0 < rank) {
+                        const float* p = L.P + (size_t)row * rank + j0;
+                        const size_t step = (size_t)args.M * rank;
+#pragma unroll 8
+                        for (int c = 0; c < L.slices; c++) {
+                            lo += *reinterpret_cast<const float4v*>(p + c * step);
+                            hi += *reinterpret_cast<const float4v*>(p + c * step + 4);
                         }
-                        w[c][s] = __builtin_bit_cast(half8, d);
+                        if (L.hidden && n0 == 0 && j0 == k0) {
+                            float4v* h = reinterpret_cast<float4v*>(L.hidden + (size_t)row * rank + j0);
+                            h[0] = lo;
+                            h[1] = hi;
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        v[s][e] = lo[e];
+                        v[s][4 + e] = hi[e];
+                        top = fmaxf(top, fmaxf(fabsf(lo[e]), fabsf(hi[e])));
+                    }
+                }
+                b.power = 1.0f;
+                if (FMT != kE3M2B) {
+                    top = fmaxf(top, __shfl_xor(top, 16, 64));
+                    top = fmaxf(top, __shfl_xor(top, 32, 64));
+                    const int exponent = exponent_for(top);
+                    b.power = power_of_two(exponent);
+                    const float down = power_of_two(-exponent);
+#pragma unroll
+                    for (int s = 0; s < JS; s++)
+#pragma unroll
+                        for (int e = 0; e < 8; e++) v[s][e] *= down;
+                }
+#pragma unroll
+                for (int s = 0; s < JS; s++) {
+                    u32x4 term[2];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        uint16_t x[2], y[2];
+                        split_terms<FMT>(v[s][2 * e], x);
+                        split_terms<FMT>(v[s][2 * e + 1], y);
+                        term[0][e] = x[0] | (uint32_t)y[0] << 16;
+                        term[1][e] = x[1] | (uint32_t)y[1] << 16;
+                    }
+                    if (PACKED) b.p[s][0] = 8 * g >= 2 * rank ? u32x4{0, 0, 0, 0} : (8 * g >= rank ? term[1] : term[0]);
+                    else {
+                        b.p[s][0] = term[0];
+                        b.p[s][TERMS - 1] = term[1];
                     }
                 }
             }
-            float4v acc[4] = {float4v{0, 0, 0, 0}, float4v{0, 0, 0, 0}, float4v{0, 0, 0, 0}, float4v{0, 0, 0, 0}};
+            const float scale = args.scaling ? args.scaling[a] : 1.0f;
 #pragma unroll
-            for (int s = 0; s < JS; s++) {
-                u32x4 term[2];
+            for (int c = 0; c < CB; c++) {
+                float4v acc[4] = {float4v{0, 0, 0, 0}, float4v{0, 0, 0, 0}, float4v{0, 0, 0, 0}, float4v{0, 0, 0, 0}};
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    uint16_t x[2], y[2];
-                    split_terms<FMT>(v[s][2 * e], x);
-                    split_terms<FMT>(v[s][2 * e + 1], y);
-                    term[0][e] = x[0] | (uint32_t)y[0] << 16;
-                    term[1][e] = x[1] | (uint32_t)y[1] << 16;
+                for (int s = 0; s < JS; s++)
+#pragma unroll
+                    for (int k = 0; k < TERMS; k++)
+#pragma unroll
+                        for (int t4 = 0; t4 < 4; t4++)
+                            acc[t4] = mfma16x16x32_of<FMT>(__builtin_bit_cast(half8, w[c][t4][s]), __builtin_bit_cast(half8, b.p[s][k]), acc[t4]);
+                if (b.mine == a) {
+#pragma unroll
+                    for (int t4 = 0; t4 < 4; t4++)
+#pragma unroll
+                        for (int p = 0; p < 2; p++) {
+                            const uint32_t d = b.y[c][t4 >> 1][2 * (t4 & 1) + p];
+                            const float lo = to_float<FMT>((uint16_t)d) + acc[t4][2 * p] * b.power * scale;
+                            const float hi = to_float<FMT>((uint16_t)(d >> 16)) + acc[t4][2 * p + 1] * b.power * scale;
+                            b.y[c][t4 >> 1][2 * (t4 & 1) + p] = to_bits<FMT>(lo) | (uint32_t)to_bits<FMT>(hi) << 16;
+                        }
+                    store = true;
                 }
-                if (PACKED) {
-                    const half8 both = __builtin_bit_cast(half8, 8 * g >= rank ? term[1] : term[0]);
-#pragma unroll
-                    for (int c = 0; c < 4; c++) acc[c] = mfma16x16x32_of<FMT>(w[c][s], both, acc[c]);
-                } else {
-#pragma unroll
-                    for (int p = 0; p < 2; p++)
-#pragma unroll
-                        for (int c = 0; c < 4; c++) acc[c] = mfma16x16x32_of<FMT>(w[c][s], __builtin_bit_cast(half8, term[p]), acc[c]);
-                }
-            }
-            if (mine == a) {
-                const float up = FMT != kE3M2B ? power_of_two(exponent) : 1.0f, s = args.scaling ? args.scaling[a] : 1.0f;
-                u32x4 y[2];
-                y[0] = *reinterpret_cast<const u32x4*>(L.Y + where);
-                y[1] = *reinterpret_cast<const u32x4*>(L.Y + where + 8);
-#pragma unroll
-                for (int c = 0; c < 4; c++)
-#pragma unroll
-                    for (int p = 0; p < 2; p++) {
-                        const uint32_t d = y[c >> 1][2 * (c & 1) + p];
-                        const float lo = to_float<FMT>((uint16_t)d) + acc[c][2 * p] * up * s;
-                        const float hi = to_float<FMT>((uint16_t)(d >> 16)) + acc[c][2 * p + 1] * up * s;
-                        y[c >> 1][2 * (c & 1) + p] = to_bits<FMT>(lo) | (uint32_t)to_bits<FMT>(hi) << 16;
-                    }
-                *reinterpret_cast<u32x4*>(L.out + where) = y[0];
-                *reinterpret_cast<u32x4*>(L.out + where + 8) = y[1];
             }
         }
+        if (store) {
+            uint16_t* to = L.out + (size_t)row * D + n0 + 8 * g;
+#pragma unroll
+            for (int c = 0; c < CB; c++)
+                if (n0 + 64 * c < D) {
+                    *reinterpret_cast<u32x4*>(to + 64 * c) = b.y[c][0];
+                    *reinterpret_cast<u32x4*>(to + 64 * c + 32) = b.y[c][1];
+                }
+        }
+    };
+
+    if (SLICED) {
+        Rows b;
+        for (int64_t t = 0; t < tiles; t++) {
+            load(b, t);
+            work(b, t);
+        }
+    } else {
+        // the next row tile is in flight while one is worked on (past the end: the last one again, not stored)
+        Rows b[2];
+        load(b[0], 0);
+        if (args.adapters == 1) hold(0);
+        for (int64_t t = 0; t < tiles; t += 2) {
+            load(b[1], min(t + 1, tiles - 1));
+            work(b[0], t);
+            if (t + 1 >= tiles) break;
+            load(b[0], min(t + 2, tiles - 1));
+            work(b[1], t + 1);
+        }
     }
+}
+
+template <int FMT, int JS, bool PACKED, bool TURNED, bool SLICED, int CB>
+__global__ __launch_bounds__(256) void lora_expand_kernel(ExpandArgs args)
+{
+    __shared__ __align__(16) unsigned char shared[kExpandLds<TURNED>];
+    expand_block<FMT, JS, PACKED, TURNED, SLICED, CB>(args, blockIdx.x, blockIdx.y, shared);
 }
 
 // ------------------------------------------------------------------ outer
@@ -372,89 +559,133 @@ struct OuterArgs {
 
 constexpr int kChunk = 64;      // rows between two barriers
 
+template <int FMT, int JT, int CT>
+struct OuterLds {
+    static constexpr int TERMS = FMT == kE3M2B ? 3 : 2, kCols = 64 * CT, kLdQ = kCols + 16, kLdP = kChunk + 8;
+    uint16_t q[kChunk * kLdQ];
+    uint16_t p[TERMS][16 * JT][kLdP];
+    uint32_t top[16 * JT];
+    float up[16 * JT];
+};
+
 // G[a][j][c] = sum over the adapter's rows m of P[m][j] Q[m][c].  A workgroup: one adapter, 64 * CT columns, one range of rows, a
 // chunk of 64 rows at a time: the rows of Q go to LDS as they are and are read back turned, P is split into 16-bit terms and stored
-// turned.  fp16: two terms, and a power of two per chunk and column of P, its products are added up per chunk; bf16: three terms.
-// Rows of other adapters count as zeros on both sides (an infinity in one of them does not reach this sum).
+// turned, while the next chunk is on its way.  fp16: two terms, and a power of two per chunk and column of P, its products are added
+// up per chunk; bf16: three terms.  Rows of other adapters count as zeros on both sides (an infinity in one of them does not reach this
+// sum), chunks without a row of this one are passed over.
 template <int FMT, int JT, int CT, bool BY_COLUMN>
-__global__ __launch_bounds__(256) void lora_outer_kernel(OuterArgs args)
+__device__ __forceinline__ void outer_block(const OuterArgs& args, int block, int a, OuterLds<FMT, JT, CT>& lds)
 {
-    constexpr int TERMS = FMT == kE3M2B ? 3 : 2;
-    constexpr int kCols = 64 * CT, kLdQ = kCols + 16, kLdP = kChunk + 8;       // elements between two rows in LDS
+    using Lds = OuterLds<FMT, JT, CT>;
+    constexpr int TERMS = Lds::TERMS, kCols = Lds::kCols, kLdQ = Lds::kLdQ;
     constexpr int kQv = kChunk * kCols / 8 / 256;                              // 16-byte pieces of Q a thread
     constexpr int kPv = JT;                                                    // float4 of P a thread
-    __shared__ __align__(16) uint16_t q_lds[kChunk * kLdQ];
-    __shared__ __align__(16) uint16_t p_lds[TERMS][16 * JT][kLdP];
-    __shared__ uint32_t top[16 * JT];
-    __shared__ __align__(16) float up[16 * JT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
-    const int a = blockIdx.y, rank = args.rank, C = args.C, per_row = rank / 4;
-    const int blocks = (C + kCols - 1) / kCols, split = (int)blockIdx.x / blocks, c0 = ((int)blockIdx.x % blocks) * kCols;
+    const int rank = args.rank, C = args.C, per_row = rank / 4;
+    const int blocks = (C + kCols - 1) / kCols, split = block / blocks, c0 = (block % blocks) * kCols;
     const int chunks = (int)((args.M + kChunk - 1) / kChunk);
     const int begin = slice_begin(chunks, args.splits, split), end = slice_begin(chunks, args.splits, split + 1);
     const float s = args.scaling ? args.scaling[a] : 1.0f;
+    const bool even = (per_row & (per_row - 1)) == 0;                          // lanes of the same columns lie a power of two apart
+
+    int prow[kPv], pj[kPv];
+#pragma unroll
+    for (int v = 0; v < kPv; v++) {
+        const int f = threadIdx.x + 256 * v;
+        prow[v] = f / per_row;
+        pj[v] = (f % per_row) * 4;
+    }
+    const int qcol = (threadIdx.x % (kCols / 8)) * 8, qrow = threadIdx.x / (kCols / 8);
+    constexpr int kQstep = 256 / (kCols / 8);
 
     float4v sum[JT][CT];
 #pragma unroll
     for (int j = 0; j < JT; j++)
 #pragma unroll
         for (int c = 0; c < CT; c++) sum[j][c] = float4v{0, 0, 0, 0};
-    for (int chunk = begin; chunk < end; chunk++) {
+
+    auto owner = [&](int chunk) { return adapter_of(args.index, (int64_t)chunk * kChunk + lane, args.M, args.adapters); };
+    int ahead = begin < end ? owner(begin) : kNoAdapter;          // of chunk `next`
+    int next = begin;
+    auto find = [&](uint64_t& rows) {                             // the next chunk with rows of this adapter, or end
+        while (next < end) {
+            const int chunk = next++;
+            rows = __ballot(ahead == a);
+            if (next < end) ahead = owner(next);
+            if (rows) return chunk;
+        }
+        return end;
+    };
+    u32x4 q[kQv];
+    float4v p4[kPv];
+    auto load = [&](int chunk, uint64_t rows) {
         const int64_t m0 = (int64_t)chunk * kChunk;
-        const uint64_t rows = __ballot(adapter_of(args.index, m0 + lane, args.M, args.adapters) == a);
-        if (!rows) continue;                                  // (the same in every wavefront)
-        u32x4 q[kQv];
+        const uint16_t* from = args.Q + (size_t)m0 * C + c0 + qcol;
 #pragma unroll
         for (int v = 0; v < kQv; v++) {
-            const int p = threadIdx.x + 256 * v, row = p / (kCols / 8), col = c0 + (p % (kCols / 8)) * 8;
+            const int row = qrow + kQstep * v;
             q[v] = u32x4{0, 0, 0, 0};
-            if (((rows >> row) & 1) && col < C) q[v] = *reinterpret_cast<const u32x4*>(args.Q + (size_t)(m0 + row) * C + col);
+            if (((rows >> row) & 1) && c0 + qcol < C) q[v] = *reinterpret_cast<const u32x4*>(from + (size_t)row * C);
         }
-        float4v p4[kPv];
 #pragma unroll
         for (int v = 0; v < kPv; v++) {
-            const int f = threadIdx.x + 256 * v, row = f / per_row, j = (f % per_row) * 4;
             p4[v] = float4v{0, 0, 0, 0};
-            if (row < kChunk && ((rows >> row) & 1)) {
-                for (int c = 0; c < args.slices; c++)
-                    p4[v] += *reinterpret_cast<const float4v*>(args.P + ((size_t)c * args.M + m0 + row) * rank + j);
+            if (prow[v] < kChunk && ((rows >> prow[v]) & 1)) {
+                const float* at = args.P + (size_t)(m0 + prow[v]) * rank + pj[v];
+#pragma unroll 4
+                for (int c = 0; c < args.slices; c++) p4[v] += *reinterpret_cast<const float4v*>(at + (size_t)c * args.M * rank);
             }
         }
-        __syncthreads();                                      // (the last chunk's operands have been read)
+    };
+    uint64_t rows = 0;
+    int chunk = find(rows);
+    if (chunk < end) load(chunk, rows);
+    while (chunk < end) {
+        __syncthreads();                                          // (the last chunk's operands have been read)
         if (FMT != kE3M2B) {
-            if (threadIdx.x < 16 * JT) top[threadIdx.x] = 0;
+            if (threadIdx.x < 16 * JT) lds.top[threadIdx.x] = 0;
             __syncthreads();
 #pragma unroll
             for (int v = 0; v < kPv; v++) {
-                const int f = threadIdx.x + 256 * v, row = f / per_row, j = (f % per_row) * 4;
-                if (row < kChunk)
+                uint32_t m[4];                                    // (magnitudes order like their bits, NaN above all)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) atomicMax(&top[j + e], __builtin_bit_cast(uint32_t, fabsf(p4[v][e])));
+                for (int e = 0; e < 4; e++) {
+                    const float x = fabsf(p4[v][e]);
+                    m[e] = __builtin_bit_cast(uint32_t, x);
+                }
+                if (even) {
+                    for (int off = per_row; off < 64; off <<= 1) {
+#pragma unroll
+                        for (int e = 0; e < 4; e++) m[e] = max(m[e], (uint32_t)__shfl_xor((int)m[e], off, 64));
+                    }
+                }
+                if (prow[v] < kChunk && (!even || lane < per_row)) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) atomicMax(&lds.top[pj[v] + e], m[e]);
+                }
             }
             __syncthreads();
-            if (threadIdx.x < 16 * JT) up[threadIdx.x] = power_of_two(exponent_for(__builtin_bit_cast(float, top[threadIdx.x])));
+            if (threadIdx.x < 16 * JT) lds.up[threadIdx.x] = power_of_two(exponent_for(__builtin_bit_cast(float, lds.top[threadIdx.x])));
         }
 #pragma unroll
-        for (int v = 0; v < kQv; v++) {
-            const int p = threadIdx.x + 256 * v, row = p / (kCols / 8), col = (p % (kCols / 8)) * 8;
-            *reinterpret_cast<u32x4*>(q_lds + row * kLdQ + col) = q[v];
-        }
+        for (int v = 0; v < kQv; v++) *reinterpret_cast<u32x4*>(lds.q + (qrow + kQstep * v) * kLdQ + qcol) = q[v];
 #pragma unroll
         for (int v = 0; v < kPv; v++) {
-            const int f = threadIdx.x + 256 * v, row = f / per_row, j = (f % per_row) * 4;
-            if (row < kChunk)
+            if (prow[v] < kChunk)
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     uint16_t t[TERMS];
                     float x = p4[v][e];
-                    if (FMT != kE3M2B) x *= power_of_two(-exponent_for(__builtin_bit_cast(float, top[j + e])));
+                    if (FMT != kE3M2B) x *= power_of_two(-exponent_for(__builtin_bit_cast(float, lds.top[pj[v] + e])));
                     split_terms<FMT>(x, t);
 #pragma unroll
-                    for (int k = 0; k < TERMS; k++) p_lds[k][j + e][row] = t[k];
+                    for (int k = 0; k < TERMS; k++) lds.p[k][pj[v] + e][prow[v]] = t[k];
                 }
         }
         __syncthreads();
+        chunk = find(rows);
+        if (chunk < end) load(chunk, rows);
         float4v part[JT][CT];
         float4v (&acc)[JT][CT] = FMT == kE3M2B ? sum : part;
         if (FMT != kE3M2B) {
@@ -469,16 +700,13 @@ __global__ __launch_bounds__(256) void lora_outer_kernel(OuterArgs args)
 #pragma unroll
             for (int j = 0; j < JT; j++)
 #pragma unroll
-                for (int k = 0; k < TERMS; k++) p[j][k] = *reinterpret_cast<const half8*>(&p_lds[k][16 * j + i][32 * step + 8 * g]);
+                for (int k = 0; k < TERMS; k++) p[j][k] = *reinterpret_cast<const half8*>(&lds.p[k][16 * j + i][32 * step + 8 * g]);
 #pragma unroll
             for (int c = 0; c < CT; c++) {
-                typedef short s4 __attribute__((ext_vector_type(4)));
                 u32x4 d;
 #pragma unroll
                 for (int e = 0; e < 2; e++) {
-                    const int row = 32 * step + 8 * g + 4 * e + (i >> 2), col = (wave * CT + c) * 16 + 4 * (i & 3);
-                    const s4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)(q_lds + row * kLdQ + col));
-                    const u32x2 b = __builtin_bit_cast(u32x2, r);
+                    const u32x2 b = read_turned(lds.q + (32 * step + 8 * g + 4 * e + (i >> 2)) * kLdQ + (wave * CT + c) * 16 + 4 * (i & 3));
                     d[2 * e] = b[0];
                     d[2 * e + 1] = b[1];
                 }
@@ -491,7 +719,7 @@ __global__ __launch_bounds__(256) void lora_outer_kernel(OuterArgs args)
         if (FMT != kE3M2B) {
 #pragma unroll
             for (int j = 0; j < JT; j++) {
-                const float4v f = *reinterpret_cast<const float4v*>(up + 16 * j + 4 * g);
+                const float4v f = *reinterpret_cast<const float4v*>(lds.up + 16 * j + 4 * g);
 #pragma unroll
                 for (int c = 0; c < CT; c++) sum[j][c] += part[j][c] * f;
             }
@@ -520,6 +748,13 @@ __global__ __launch_bounds__(256) void lora_outer_kernel(OuterArgs args)
         }
 }
 
+template <int FMT, int JT, int CT, bool BY_COLUMN>
+__global__ __launch_bounds__(256) void lora_outer_kernel(OuterArgs args)
+{
+    __shared__ __align__(16) OuterLds<FMT, JT, CT> lds;
+    outer_block<FMT, JT, CT, BY_COLUMN>(args, blockIdx.x, blockIdx.y, lds);
+}
+
 // out[k] (+)= the sum over the splits, in their order; two tensors in one launch
 struct JoinArgs {
     const float4v* part[2];
@@ -535,6 +770,7 @@ __global__ __launch_bounds__(256) void lora_join_kernel(JoinArgs args)
         const int w = k >= args.count[0];
         const int64_t e = w ? k - args.count[0] : k;
         float4v v = args.accumulate ? args.out[w][e] : float4v{0, 0, 0, 0};
+        #pragma unroll 8
         for (int c = 0; c < args.splits[w]; c++) v += args.part[w][(size_t)c * args.count[w] + e];
         args.out[w][e] = v;
     }
@@ -543,6 +779,10 @@ __global__ __launch_bounds__(256) void lora_join_kernel(JoinArgs args)
 // ------------------------------------------------------------------ plans and launches
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Up to this many rows the slices of a shrink are added up by the kernels that read them, and the adapters of the rows are dealt to workgroups of their own;
+// above it a launch of its own adds them up.
+constexpr int64_t kFewRows = 64;
+
 // Rows a shrink workgroup takes, slots its adapters are dealt to, and slices of the contraction: two workgroups for each compute unit
 // where the contraction is long enough to be cut (a slice gives each of the four wavefronts at least one unit of 64).
 struct ShrinkPlan {
@@ -550,17 +790,17 @@ struct ShrinkPlan {
     int64_t groups;
 };
 
-static ShrinkPlan plan_shrink(int64_t M, int C, int adapters, bool indexed)
+static ShrinkPlan plan_shrink(int64_t M, int C, int rank, int adapters)
 {
     ShrinkPlan p;
-    p.row_tiles = M > 64 ? 2 : 1;
+    p.row_tiles = M <= kFewRows ? 1 : (rank > 64 ? 2 : 4);
     const int64_t rows = 16 * p.row_tiles;
     p.groups = ceil_div(M, rows);
-    p.slots = indexed && M <= 64 ? (int)(adapters < rows ? adapters : rows) : 1;
+    p.slots = M <= kFewRows ? (int)(adapters < rows ? adapters : rows) : 1;
     const int64_t have = p.groups * p.slots, most = C / 64 >= 8 ? C / 256 : 1;
     int64_t slices = ceil_div(512, have);
     if (slices > most) slices = most;
-    if (slices > 32) slices = 32;
+    if (slices > 16) slices = 16;
     p.slices = (int)(slices < 1 ? 1 : slices);
     return p;
 }
@@ -576,40 +816,56 @@ static int plan_splits(int64_t M, int C, int cols, int adapters)
 
 static int outer_columns(int rank) { return rank > 64 ? 128 : 256; }
 
-template <int FMT, int RT, bool TURNED>
-static void launch_shrink_rank(const ShrinkArgs& a, int rank, dim3 grid, hipStream_t stream)
-{
-    if (rank <= 16) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, RT, TURNED>), grid, dim3(256), 0, stream, a);
-    else if (rank <= 32) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, RT, TURNED>), grid, dim3(256), 0, stream, a);
-    else if (rank <= 64) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, RT, TURNED>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 8, RT, TURNED>), grid, dim3(256), 0, stream, a);
-}
-
 template <int FMT, bool TURNED>
-static hipError_t launch_shrink(ShrinkArgs& a, int row_tiles, int64_t workgroups, hipStream_t stream)
+static hipError_t launch_shrink(const ShrinkArgs& a, bool few, int64_t workgroups, hipStream_t stream)
 {
     int rank = 0;
     for (int l = 0; l < a.layers; l++) rank = a.layer[l].rank > rank ? a.layer[l].rank : rank;
-    const dim3 grid((unsigned)workgroups, (unsigned)a.slots);
-    if (row_tiles == 1) launch_shrink_rank<FMT, 1, TURNED>(a, rank, grid, stream);
-    else launch_shrink_rank<FMT, 2, TURNED>(a, rank, grid, stream);
+    const dim3 grid((unsigned)workgroups, (unsigned)a.slots), block(256);
+    if (few) {
+        if (rank <= 16) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 1, TURNED>), grid, block, 0, stream, a);
+        else if (rank <= 32) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 1, TURNED>), grid, block, 0, stream, a);
+        else if (rank <= 64) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, 1, TURNED>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 8, 1, TURNED>), grid, block, 0, stream, a);
+    } else {
+        if (rank <= 16) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 4, TURNED>), grid, block, 0, stream, a);
+        else if (rank <= 32) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 4, TURNED>), grid, block, 0, stream, a);
+        else if (rank <= 64) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, 4, TURNED>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 8, 2, TURNED>), grid, block, 0, stream, a);
+    }
     return hipGetLastError();
 }
 
-template <int FMT, bool TURNED>
-static hipError_t launch_expand(ExpandArgs& a, int64_t workgroups, hipStream_t stream)
+template <int FMT>
+static hipError_t launch_finish(const float* P, float* sum, uint16_t* terms, float* power, int64_t M, int rank, int slices, hipStream_t stream)
 {
-    int rank = 0;
+    int lanes = 2;
+    while (4 * lanes < rank) lanes *= 2;
+    const FinishArgs f{P, sum, terms, power, M, rank, slices, lanes};
+    hipLaunchKernelGGL(lora_finish_kernel<FMT>, dim3((unsigned)ceil_div(M * lanes, 256)), dim3(256), 0, stream, f);
+    return hipGetLastError();
+}
+
+// 64-wide blocks of columns that a wavefront of the expand kernel takes side by side
+static int expand_blocks(bool few, int rank) { return few || rank > 64 ? 1 : 2; }
+
+template <int FMT, bool TURNED>
+static hipError_t launch_expand(const ExpandArgs& a, bool few, int rank, int64_t workgroups, hipStream_t stream)
+{
+    const dim3 grid((unsigned)workgroups, (unsigned)a.slots), block(256);
     bool packed = true;
-    for (int l = 0; l < a.layers; l++) {
-        rank = a.layer[l].rank > rank ? a.layer[l].rank : rank;
-        packed = packed && a.layer[l].rank <= 16;
+    for (int l = 0; l < a.layers; l++) packed = packed && a.layer[l].rank <= 16;
+    if (few) {
+        if (packed) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, true, TURNED, true, 1>), grid, block, 0, stream, a);
+        else if (rank <= 32) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, false, TURNED, true, 1>), grid, block, 0, stream, a);
+        else if (rank <= 64) hipLaunchKernelGGL((lora_expand_kernel<FMT, 2, false, TURNED, true, 1>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((lora_expand_kernel<FMT, 4, false, TURNED, true, 1>), grid, block, 0, stream, a);
+    } else {
+        if (packed) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, true, TURNED, false, 2>), grid, block, 0, stream, a);
+        else if (rank <= 32) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, false, TURNED, false, 2>), grid, block, 0, stream, a);
+        else if (rank <= 64) hipLaunchKernelGGL((lora_expand_kernel<FMT, 2, false, TURNED, false, 2>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((lora_expand_kernel<FMT, 4, false, TURNED, false, 1>), grid, block, 0, stream, a);
     }
-    const dim3 grid((unsigned)workgroups, (unsigned)a.slots);
-    if (packed) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, true, TURNED>), grid, dim3(256), 0, stream, a);
-    else if (rank <= 32) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, false, TURNED>), grid, dim3(256), 0, stream, a);
-    else if (rank <= 64) hipLaunchKernelGGL((lora_expand_kernel<FMT, 2, false, TURNED>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((lora_expand_kernel<FMT, 4, false, TURNED>), grid, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -624,21 +880,47 @@ static hipError_t launch_outer(const OuterArgs& a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Row tiles of 16 rows that an expand workgroup takes one after another (its operands of W stay in registers): four from the point
-// on where enough workgroups remain.
-static int expand_row_tiles(int64_t M, int64_t columns)
+// Row tiles of 16 rows that an expand workgroup takes one after another (its operands of W stay in registers, and the next tile's loads are in
+// flight): as many as leave four workgroups for each compute unit, eight at most.
+static int expand_row_tiles(int64_t M, int64_t column_blocks)
 {
-    const int64_t tiles = ceil_div(M, 16), have = tiles * ceil_div(columns, 256);
-    return have >= 4096 ? 4 : (have >= 2048 ? 2 : 1);
+    if (M <= kFewRows) return 1;
+    const int64_t tiles = ceil_div(M, 16), t = tiles * column_blocks / 1024;
+    return (int)(t < 1 ? 1 : (t > 8 ? 8 : t));
 }
 
 static size_t round_up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
+// What lies behind the zero region for one shrink: the slices; with more than a few rows the terms and powers of two made of them.
+struct ShrinkSpace {
+    size_t slices, terms, power, bytes;
+};
+
+static ShrinkSpace shrink_space(const ShrinkPlan& p, int64_t M, int64_t rank)
+{
+    ShrinkSpace s{};
+    s.slices = round_up((size_t)p.slices * M * rank * 4);
+    if (M > kFewRows) {
+        s.terms = round_up((size_t)M * rank * 4);
+        s.power = round_up((size_t)M * 4);
+    }
+    s.bytes = s.slices + s.terms + s.power;
+    return s;
+}
+
+// The rank that decides which kernels run: the largest of the group.
+static int group_rank(const fp6_lora_problem* pr, int count)
+{
+    int rank = 0;
+    for (int l = 0; l < count; l++) rank = (int)pr[l].rank > rank ? (int)pr[l].rank : rank;
+    return rank;
+}
+
 size_t lora_workspace(int64_t M, const fp6_lora_problem* pr, int count, int adapters)
 {
     size_t need = kZeroBytes;
-    for (int l = 0; l < count; l++)
-        need += round_up((size_t)plan_shrink(M, (int)pr[l].K, adapters, adapters > 1).slices * M * pr[l].rank * 4);
+    const int rank = group_rank(pr, count);
+    for (int l = 0; l < count; l++) need += shrink_space(plan_shrink(M, (int)pr[l].K, rank, adapters), M, pr[l].rank).bytes;
     return need;
 }
 
@@ -653,24 +935,29 @@ static hipError_t launch_lora_t(int64_t M, const fp6_lora_problem* pr, int count
     s.index = e.index = index;
     e.scaling = scaling;
     s.adapters = e.adapters = adapters;
+    const bool few = M <= kFewRows;
+    const int rank = group_rank(pr, count), across = 256 * expand_blocks(few, rank);
     unsigned char* at = workspace + kZeroBytes;
     int64_t shrinks = 0, expands = 0, columns = 0;
-    int row_tiles = 1;
-    for (int l = 0; l < count; l++) columns += pr[l].N;
+    for (int l = 0; l < count; l++) columns += ceil_div(pr[l].N, across);
     e.row_tiles = expand_row_tiles(M, columns);
     for (int l = 0; l < count; l++) {
-        const ShrinkPlan p = plan_shrink(M, (int)pr[l].K, adapters, adapters > 1);
+        const ShrinkPlan p = plan_shrink(M, (int)pr[l].K, rank, adapters);
+        const ShrinkSpace space = shrink_space(p, M, pr[l].rank);
         s.slots = e.slots = p.slots;
-        row_tiles = p.row_tiles;
         s.layer[l] = ShrinkLayer{pr[l].X, pr[l].A, (float*)at, (int)pr[l].K, (int)pr[l].rank, p.slices, (int)shrinks};
-        e.layer[l] = ExpandLayer{(const float*)at, pr[l].B, pr[l].Y, pr[l].out, pr[l].hidden, (int)pr[l].N, (int)pr[l].rank, p.slices, (int)expands};
-        at += round_up((size_t)p.slices * M * pr[l].rank * 4);
+        e.layer[l] = ExpandLayer{few ? (const float*)at : (const float*)(at + space.slices + space.terms), (const uint16_t*)(at + space.slices),
+                                 pr[l].B, pr[l].Y, pr[l].out, pr[l].hidden, (int)pr[l].N, (int)pr[l].rank, p.slices, (int)expands};
+        at += space.bytes;
         shrinks += p.groups * p.slices;
-        expands += ceil_div(pr[l].N, 256) * ceil_div(ceil_div(M, 16), e.row_tiles);
+        expands += ceil_div(pr[l].N, across) * ceil_div(ceil_div(M, 16), e.row_tiles);
     }
-    const hipError_t err = launch_shrink<FMT, false>(s, row_tiles, shrinks, stream);
+    hipError_t err = launch_shrink<FMT, false>(s, few, shrinks, stream);
+    for (int l = 0; l < count && !few && err == hipSuccess; l++)
+        err = launch_finish<FMT>(s.layer[l].P, pr[l].hidden, const_cast<uint16_t*>(e.layer[l].terms), const_cast<float*>(e.layer[l].P), M,
+                                 (int)pr[l].rank, s.layer[l].slices, stream);
     if (err != hipSuccess) return err;
-    return launch_expand<FMT, false>(e, expands, stream);
+    return launch_expand<FMT, false>(e, few, rank, expands, stream);
 }
 
 hipError_t launch_lora(bool bf16, int64_t M, const fp6_lora_problem* pr, int count, int adapters, const int32_t* index, const float* scaling,
@@ -680,20 +967,22 @@ hipError_t launch_lora(bool bf16, int64_t M, const fp6_lora_problem* pr, int cou
                 : launch_lora_t<kE3M2>(M, pr, count, adapters, index, scaling, (unsigned char*)workspace, stream);
 }
 
-// Workspace of the backward pass behind the zero region: the slices of dH, then the splits of dA and of dB (none where there is one).
+// Workspace of the backward pass behind the zero region: the slices of dH and what is made of them, then the splits of dA and of dB (none
+// where there is one).
 struct BackwardPlan {
     ShrinkPlan shrink;
+    ShrinkSpace space;
     int splits_a, splits_b;
-    size_t dh, da, db;       // bytes
+    size_t da, db;           // bytes
 };
 
 static BackwardPlan plan_backward(int64_t M, int64_t N, int64_t K, int rank, int adapters)
 {
     BackwardPlan p;
-    p.shrink = plan_shrink(M, (int)N, adapters, adapters > 1);
+    p.shrink = plan_shrink(M, (int)N, rank, adapters);
+    p.space = shrink_space(p.shrink, M, rank);
     p.splits_a = plan_splits(M, (int)K, outer_columns(rank), adapters);
     p.splits_b = plan_splits(M, (int)N, outer_columns(rank), adapters);
-    p.dh = round_up((size_t)p.shrink.slices * M * rank * 4);
     p.da = p.splits_a > 1 ? round_up((size_t)p.splits_a * adapters * rank * K * 4) : 0;
     p.db = p.splits_b > 1 ? round_up((size_t)p.splits_b * adapters * rank * N * 4) : 0;
     return p;
@@ -702,16 +991,20 @@ static BackwardPlan plan_backward(int64_t M, int64_t N, int64_t K, int rank, int
 size_t lora_backward_workspace(int64_t M, int64_t N, int64_t K, int rank, int adapters)
 {
     const BackwardPlan p = plan_backward(M, N, K, rank, adapters);
-    return kZeroBytes + p.dh + p.da + p.db;
+    return kZeroBytes + p.space.bytes + p.da + p.db;
 }
 
 template <int FMT>
 static hipError_t launch_backward_t(const LoraBackward& b, unsigned char* workspace, hipStream_t stream)
 {
     const BackwardPlan p = plan_backward(b.M, b.N, b.K, b.rank, b.adapters);
-    float* dh = (float*)(workspace + kZeroBytes);
-    float* da = (float*)(workspace + kZeroBytes + p.dh);
-    float* db = (float*)(workspace + kZeroBytes + p.dh + p.da);
+    const bool few = b.M <= kFewRows;
+    unsigned char* at = workspace + kZeroBytes;
+    float* dh = (float*)at;
+    uint16_t* terms = (uint16_t*)(at + p.space.slices);
+    float* power = (float*)(at + p.space.slices + p.space.terms);
+    float* da = (float*)(at + p.space.bytes);
+    float* db = (float*)(at + p.space.bytes + p.da);
     ShrinkArgs s{};
     s.layers = 1;
     s.M = b.M;
@@ -720,25 +1013,30 @@ static hipError_t launch_backward_t(const LoraBackward& b, unsigned char* worksp
     s.adapters = b.adapters;
     s.slots = p.shrink.slots;
     s.layer[0] = ShrinkLayer{b.dY, b.B, dh, (int)b.N, b.rank, p.shrink.slices, 0};
-    hipError_t err = launch_shrink<FMT, true>(s, p.shrink.row_tiles, p.shrink.groups * p.shrink.slices, stream);
+    hipError_t err = launch_shrink<FMT, true>(s, few, p.shrink.groups * p.shrink.slices, stream);
+    if (err != hipSuccess) return err;
+    // (right behind the shrink: what the last-level cache still holds of dY is read from there)
+    const OuterArgs ob{b.hidden, b.dY, p.splits_b > 1 ? db : b.dB, b.M, (int)b.N, b.rank, 1, b.adapters, p.splits_b, b.accumulate, b.index, b.scaling};
+    err = launch_outer<FMT, true>(ob, stream);
+    if (err != hipSuccess) return err;
+    // the sum over the slices goes where the first slice lies
+    if (!few) err = launch_finish<FMT>(dh, dh, terms, power, b.M, b.rank, p.shrink.slices, stream);
     if (err != hipSuccess) return err;
     if (b.out) {
+        const int across = 256 * expand_blocks(few, b.rank);
         ExpandArgs e{};
         e.layers = 1;
         e.M = b.M;
         e.index = b.index;
         e.adapters = b.adapters;
         e.slots = p.shrink.slots;
-        e.row_tiles = expand_row_tiles(b.M, b.K);
-        e.layer[0] = ExpandLayer{dh, b.A, b.dX, b.out, nullptr, (int)b.K, b.rank, p.shrink.slices, 0};
-        err = launch_expand<FMT, true>(e, ceil_div(b.K, 256) * ceil_div(ceil_div(b.M, 16), e.row_tiles), stream);
+        e.row_tiles = expand_row_tiles(b.M, ceil_div(b.K, across));
+        e.layer[0] = ExpandLayer{few ? dh : power, terms, b.A, b.dX, b.out, nullptr, (int)b.K, b.rank, p.shrink.slices, 0};
+        err = launch_expand<FMT, true>(e, few, b.rank, ceil_div(b.K, across) * ceil_div(ceil_div(b.M, 16), e.row_tiles), stream);
         if (err != hipSuccess) return err;
     }
-    const OuterArgs oa{dh, b.X, p.splits_a > 1 ? da : b.dA, b.M, (int)b.K, b.rank, p.shrink.slices, b.adapters, p.splits_a, b.accumulate, b.index, nullptr};
+    const OuterArgs oa{dh, b.X, p.splits_a > 1 ? da : b.dA, b.M, (int)b.K, b.rank, few ? p.shrink.slices : 1, b.adapters, p.splits_a, b.accumulate, b.index, nullptr};
     err = launch_outer<FMT, false>(oa, stream);
-    if (err != hipSuccess) return err;
-    const OuterArgs ob{b.hidden, b.dY, p.splits_b > 1 ? db : b.dB, b.M, (int)b.N, b.rank, 1, b.adapters, p.splits_b, b.accumulate, b.index, b.scaling};
-    err = launch_outer<FMT, true>(ob, stream);
     if (err != hipSuccess || (p.splits_a == 1 && p.splits_b == 1)) return err;
     JoinArgs j{};
     j.accumulate = b.accumulate;
