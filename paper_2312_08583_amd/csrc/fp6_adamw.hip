@@ -16,17 +16,17 @@ namespace fp6 {
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-// 32 bits from the number of an element, the step and the seed: two rounds of xor-shift and multiplication (by the fractional
+// 32 bits from x = number of the element * 0x9E3779B1 + t * 0x3C6EF373 + seed: two rounds of xor-shift and multiplication (by the fractional
 // parts of the golden ratio and of the roots of 5, 2 and 3).
-__device__ __forceinline__ uint32_t counter_hash(uint32_t id, uint32_t salt)
+__device__ __forceinline__ uint32_t counter_hash(uint32_t x)
 {
-    uint32_t x = id * 0x9E3779B1u + salt;
     x = (x ^ (x >> 16)) * 0x6A09E667u;
     x = (x ^ (x >> 15)) * 0xBB67AE85u;
     return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ float two_to(int e) { return e >= -126 ? __builtin_bit_cast(float, (uint32_t)(e + 127) << 23) : 0x1p-127f; }
+// 2^e for e in -127 .. 128 (2^128: 2^127, for an empty block)
+__device__ __forceinline__ float two_to(int e) { return e >= -126 ? __builtin_bit_cast(float, (uint32_t)min(e + 127, 254) << 23) : 0x1p-127f; }
 
 // The exponent of a block whose largest magnitude is `top`: -127 for an empty block.
 __device__ __forceinline__ int block_exponent(float top)
@@ -37,13 +37,15 @@ __device__ __forceinline__ int block_exponent(float top)
 }
 
 // x * 2^-e to an e4m3 code; `noise` in 0 .. 65535 decides between the neighbours; `least`: the smallest code that a nonzero x may get.
-__device__ __forceinline__ uint32_t encode(float x, float down, uint32_t noise, int least)
+// y in units of its last kept bit (2^-9 below 2^-6) plus the noise's fraction, cut: a product by a power of two and one addition, as the
+// definition has it.  An infinity or NaN becomes NaN.
+__device__ __forceinline__ uint32_t encode(float x, float down, uint32_t noise, uint32_t least)
 {
     const float y = fabsf(x) * down;
-    const int ey = max((int)(__builtin_bit_cast(uint32_t, y) >> 23) - 127, -6);
-    int k = (int)floorf(y * two_to(3 - ey) + (float)noise * 0x1p-16f);
-    if (x != 0.0f) k = max(k, least);
-    const uint32_t code = y < 0x1p9f ? (uint32_t)(((ey + 6) << 3) + k) : 0x7Fu;          // an infinity or NaN: NaN
+    const uint32_t exponent = max(__builtin_bit_cast(uint32_t, y) >> 23, 121u);
+    uint32_t k = (uint32_t)__builtin_fmaf((float)noise, 0x1p-16f, __builtin_ldexpf(y, 130 - (int)exponent));
+    if (least) k = max(k, x != 0.0f ? least : 0u);
+    const uint32_t code = y < 0x1p9f ? (exponent << 3) + k - 121 * 8 : 0x7Fu;
     return code | (__builtin_bit_cast(uint32_t, x) >> 31) << 7;
 }
 
@@ -77,13 +79,13 @@ __device__ __forceinline__ double power(double b, uint32_t t)
     return r;
 }
 
-// Four consecutive elements of a block of 256: `n` of them exist (the last block of a tensor may be short).
-template <typename T, int W>
+// Four consecutive elements; WHOLE: all four exist, else `n` of them (the end of a tensor).
+template <bool WHOLE, typename T, int W>
 __device__ __forceinline__ void load4(const T* p, int n, T (&v)[W])
 {
     typedef T vec __attribute__((ext_vector_type(4)));
-    if (n >= 4) {
-        const vec x = *reinterpret_cast<const vec*>(p);
+    if (WHOLE) {
+        const vec x = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p));
 #pragma unroll
         for (int e = 0; e < 4; e++) v[e] = x[e];
     } else {
@@ -92,12 +94,12 @@ __device__ __forceinline__ void load4(const T* p, int n, T (&v)[W])
     }
 }
 
-template <typename T, int W>
+template <bool WHOLE, typename T, int W>
 __device__ __forceinline__ void store4(T* p, int n, const T (&v)[W])
 {
     typedef T vec __attribute__((ext_vector_type(4)));
-    if (n >= 4) {
-        *reinterpret_cast<vec*>(p) = vec{v[0], v[1], v[2], v[3]};
+    if (WHOLE) {
+        __builtin_nontemporal_store(vec{v[0], v[1], v[2], v[3]}, reinterpret_cast<vec*>(p));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; e++)
@@ -105,120 +107,213 @@ __device__ __forceinline__ void store4(T* p, int n, const T (&v)[W])
     }
 }
 
-// A workgroup walks over the items of the plan: 4096 elements of a tensor, four blocks of 256 for each of its wavefronts.
-template <int BITS, typename G, typename C>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwHeader* __restrict__ plan, int64_t items, int32_t* __restrict__ step, AdamwCall call)
+// What a lane holds of a block: four elements.
+template <int BITS, typename G>
+struct BlockIn {
+    float p[4];
+    G g[4];
+    float m[4], v[4];        // 32 bits
+    uint32_t cm, cv;         // 8 bits: four codes each, and the block's scale bytes
+    uint32_t sm, sv;
+};
+
+template <int BITS, typename G, bool WHOLE>
+__device__ __forceinline__ void load_block(const AdamwItem& it, int block, int lane, BlockIn<BITS, G>& in)
+{
+    const int at = block * 256 + 4 * lane, n = (int)it.count - at;
+    load4<WHOLE>(it.param + at, n, in.p);
+    load4<WHOLE>((const G*)it.grad + at, n, in.g);
+    if (BITS == 32) {
+        load4<WHOLE>((const float*)it.first + at, n, in.m);
+        load4<WHOLE>((const float*)it.second + at, n, in.v);
+    } else {
+        const uint8_t *m = (const uint8_t*)it.first + at, *v = (const uint8_t*)it.second + at;
+        if (WHOLE) {
+            in.cm = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(m));
+            in.cv = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(v));
+        } else {
+            in.cm = in.cv = 0;
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (e < n) {
+                    in.cm |= (uint32_t)m[e] << (8 * e);
+                    in.cv |= (uint32_t)v[e] << (8 * e);
+                }
+        }
+        in.sm = it.first_scales[block];
+        in.sv = it.second_scales[block];
+    }
+}
+
+template <int BITS, typename G, typename C, bool WHOLE>
+__device__ __forceinline__ void step_block(const AdamwItem& it, int block, int lane, const BlockIn<BITS, G>& in, const StepScalars& s)
 {
 #pragma clang fp contract(off)
-    if (call.found_inf && *call.found_inf != 0.0f) return;
-    const uint32_t t = (uint32_t)*step + 1;
-    const double lr = call.lr_device ? (double)*call.lr_device : call.lr;
+    const int at = block * 256 + 4 * lane, n = (int)it.count - at;
+    float p[4], m[4], v[4], u[4];
+    if (BITS == 32) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            m[e] = in.m[e];
+            v[e] = in.v[e];
+        }
+    } else {
+        const float sm = two_to((int)in.sm - 127), sv = two_to((int)in.sv - 127);
+        m[0] = __builtin_amdgcn_cvt_f32_fp8((int)in.cm, 0) * sm;
+        m[1] = __builtin_amdgcn_cvt_f32_fp8((int)in.cm, 1) * sm;
+        m[2] = __builtin_amdgcn_cvt_f32_fp8((int)in.cm, 2) * sm;
+        m[3] = __builtin_amdgcn_cvt_f32_fp8((int)in.cm, 3) * sm;
+        u[0] = __builtin_amdgcn_cvt_f32_fp8((int)in.cv, 0) * sv;
+        u[1] = __builtin_amdgcn_cvt_f32_fp8((int)in.cv, 1) * sv;
+        u[2] = __builtin_amdgcn_cvt_f32_fp8((int)in.cv, 2) * sv;
+        u[3] = __builtin_amdgcn_cvt_f32_fp8((int)in.cv, 3) * sv;
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = u[e] * u[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const float x = grad_of<G>(in.g[e]) * s.scale;
+        m[e] = m[e] * s.b1 + x * s.c1;
+        v[e] = v[e] * s.b2 + x * x * s.c2;
+        u[e] = __builtin_sqrtf(v[e]);
+        p[e] = in.p[e] * s.decay - m[e] / (u[e] * s.second + s.eps) * s.first;
+    }
+    store4<WHOLE>(it.param + at, n, p);
+    if (sizeof(C) == 2) {
+        C c[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) c[e] = (C)p[e];
+        store4<WHOLE>((C*)it.copy + at, n, c);
+    }
+    if (BITS == 32) {
+        store4<WHOLE>((float*)it.first + at, n, m);
+        store4<WHOLE>((float*)it.second + at, n, v);
+    } else {
+        float tm = 0.0f, tu = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (WHOLE || e < n) {
+                tm = fmaxf(tm, fabsf(m[e]));
+                tu = fmaxf(tu, u[e]);
+            }
+        const int em = block_exponent(wave_max(tm)), eu = block_exponent(wave_max(tu));
+        const float dm = two_to(-em), du = two_to(-eu);
+        const uint32_t id = (it.id + (uint32_t)at) * 0x9E3779B1u + s.salt;
+        uint32_t cm = 0, cu = 0;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint32_t noise = counter_hash(id + e * 0x9E3779B1u);
+            cm |= encode(m[e], dm, noise >> 16, 0) << (8 * e);
+            cu |= encode(u[e], du, noise & 0xFFFFu, 1) << (8 * e);
+        }
+        uint8_t *to_m = (uint8_t*)it.first + at, *to_u = (uint8_t*)it.second + at;
+        if (WHOLE) {
+            __builtin_nontemporal_store(cm, reinterpret_cast<uint32_t*>(to_m));
+            __builtin_nontemporal_store(cu, reinterpret_cast<uint32_t*>(to_u));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (e < n) {
+                    to_m[e] = (uint8_t)(cm >> (8 * e));
+                    to_u[e] = (uint8_t)(cu >> (8 * e));
+                }
+        }
+        if (lane == 0) {
+            it.first_scales[block] = (uint8_t)(em + 127);
+            it.second_scales[block] = (uint8_t)(eu + 127);
+        }
+    }
+}
+
+// A workgroup walks over the items of the plan; a wavefront takes the blocks of 256 elements wave, wave + 4, ... of an item, the next one's loads
+// in flight while it works on one.  Whole blocks take no branch; the last one of a tensor may be short.  Bound by memory: 109 million
+// elements with states in 8 bits 401 us for 1.96 GB, 4.9 TB/s (a large copy: 5.2), with 112 vector instructions an element beside it;
+// 20 million with states in 32 bits 122 us, 4.9 TB/s; 0.6 million 6.8 us, of which a plan of one block takes 5.0.
+template <int BITS, typename G, typename C>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwHeader* __restrict__ plan, const AdamwItem* __restrict__ list, int64_t items,
+                                                    int32_t* __restrict__ step, AdamwCall call)
+{
+#pragma clang fp contract(off)
     StepScalars s;
+    const uint32_t t = (uint32_t)*step + 1;
+    if (call.found_inf && *call.found_inf != 0.0f) return;
+    // (not a plan, one of the other kind, or fewer items than the caller says: nothing beyond it is touched)
+    if (plan->magic != kAdamwMagic || plan->state_bits != BITS) return;
+    items = min(items, (int64_t)plan->items);
+    s.scale = call.grad_scale ? *call.grad_scale : 1.0f;
+    const double lr = call.lr_device ? (double)*call.lr_device : call.lr;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     s.decay = (float)(1.0 - lr * call.weight_decay);
-    s.first = (float)(lr / (1.0 - power(call.beta1, t)));
-    s.second = (float)(1.0 / sqrt(1.0 - power(call.beta2, t)));
     s.b1 = (float)call.beta1;
     s.c1 = (float)(1.0 - call.beta1);
     s.b2 = (float)call.beta2;
     s.c2 = (float)(1.0 - call.beta2);
     s.eps = (float)call.eps;
-    s.scale = call.grad_scale ? *call.grad_scale : 1.0f;
     s.salt = t * 0x3C6EF373u + call.seed;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AdamwItem* list = reinterpret_cast<const AdamwItem*>(reinterpret_cast<const unsigned char*>(plan) + plan->items_at);
-    const fp6_adamw_tensor* tensors = reinterpret_cast<const fp6_adamw_tensor*>(plan + 1);
-    const uint32_t* first_block = reinterpret_cast<const uint32_t*>(reinterpret_cast<const unsigned char*>(plan) + plan->blocks_at);
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const AdamwItem it = list[item];
-        const fp6_adamw_tensor T = tensors[it.tensor];
-        const uint32_t id0 = first_block[it.tensor] * 256u;
-        const int64_t base = (int64_t)it.part * kAdamwItem + wave * (kAdamwItem / 4);
-#pragma unroll 2
-        for (int b = 0; b < kAdamwItem / 1024; b++) {
-            const int64_t block = base + b * 256;
-            if (block >= T.count) break;
-            const int64_t at = block + 4 * lane, left = T.count - at;
-            const int n = left >= 4 ? 4 : (left > 0 ? (int)left : 0);
-            float p[4], m[4], v[4], u[4];
-            G g[4];
-            load4(T.param + at, n, p);
-            load4((const G*)T.grad + at, n, g);
-            if (BITS == 32) {
-                load4((const float*)T.first + at, n, m);
-                load4((const float*)T.second + at, n, v);
-            } else {
-                uint8_t cm[4], cv[4];
-                load4((const uint8_t*)T.first + at, n, cm);
-                load4((const uint8_t*)T.second + at, n, cv);
-                const float sm = two_to((int)T.first_scales[block >> 8] - 127), sv = two_to((int)T.second_scales[block >> 8] - 127);
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    m[e] = __builtin_amdgcn_cvt_f32_fp8((int)cm[e], 0) * sm;
-                    const float r = __builtin_amdgcn_cvt_f32_fp8((int)cv[e], 0) * sv;
-                    v[e] = r * r;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const float x = grad_of<G>(g[e]) * s.scale;
-                m[e] = m[e] * s.b1 + x * s.c1;
-                v[e] = v[e] * s.b2 + x * x * s.c2;
-                u[e] = __builtin_sqrtf(v[e]);
-                p[e] = p[e] * s.decay - m[e] / (u[e] * s.second + s.eps) * s.first;
-            }
-            store4(T.param + at, n, p);
-            if (sizeof(C) == 2) {
-                C c[4];
-#pragma unroll
-                for (int e = 0; e < 4; e++) c[e] = (C)p[e];
-                store4((C*)T.copy + at, n, c);
-            }
-            if (BITS == 32) {
-                store4((float*)T.first + at, n, m);
-                store4((float*)T.second + at, n, v);
-            } else {
-                float tm = 0.0f, tu = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (e < n) {
-                        tm = fmaxf(tm, fabsf(m[e]));
-                        tu = fmaxf(tu, u[e]);
-                    }
-                const int em = block_exponent(wave_max(tm)), eu = block_exponent(wave_max(tu));
-                const float dm = em == -127 ? 0x1p127f : two_to(-em), du = eu == -127 ? 0x1p127f : two_to(-eu);
-                uint8_t cm[4], cu[4];
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const uint32_t noise = counter_hash(id0 + (uint32_t)at + e, s.salt);
-                    cm[e] = (uint8_t)encode(m[e], dm, noise >> 16, 0);
-                    cu[e] = (uint8_t)encode(u[e], du, noise & 0xFFFFu, 1);
-                }
-                store4((uint8_t*)T.first + at, n, cm);
-                store4((uint8_t*)T.second + at, n, cu);
-                if (lane == 0) {
-                    T.first_scales[block >> 8] = (uint8_t)(em + 127);
-                    T.second_scales[block >> 8] = (uint8_t)(eu + 127);
-                }
-            }
+
+    // The blocks of a wavefront one after another: `per` of each of its items.  The item after the next is asked for, the next block is in flight.
+    const int64_t mine = items > blockIdx.x ? (items - 1 - blockIdx.x) / gridDim.x + 1 : 0;
+    auto item_at = [&](int64_t k) { return list[blockIdx.x + min(k, mine - 1) * gridDim.x]; };
+    const uint32_t group = blockIdx.x % kArrivalGroups, groups = min(gridDim.x, (uint32_t)kArrivalGroups);
+    const uint32_t members = (gridDim.x - 1 - group) / kArrivalGroups + 1;
+    uint32_t arrival = 0, root = 0;
+    AdamwItem it{}, next{};
+    BlockIn<BITS, G> in[2];
+    if (mine > 0) {
+        it = item_at(0);
+        if (wave < (int)(it.count / 256)) load_block<BITS, G, true>(it, wave, lane, in[0]);
+        next = item_at(1);
+    }
+    // (behind the first loads)
+    s.first = (float)(lr / (1.0 - power(call.beta1, t)));
+    s.second = (float)(1.0 / sqrt(1.0 - power(call.beta2, t)));
+    // The step is read, and the workgroup says so; the last one to say it counts the step on.
+    __syncthreads();                     // (every wavefront has its step)
+    if (threadIdx.x == 0) {
+        arrival = __hip_atomic_fetch_add(&plan->arrived[1 + group].count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+        if (arrival == members) {
+            __hip_atomic_store(&plan->arrived[1 + group].count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            root = __hip_atomic_fetch_add(&plan->arrived[0].count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
         }
     }
-    // Every workgroup has read the step before it arrives here; the last one counts it on.
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const uint32_t old = __hip_atomic_fetch_add(&plan->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        if (old == gridDim.x - 1) {
-            __hip_atomic_store(&plan->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            *step = (int32_t)t;
+    int turn = 0;
+    for (int64_t k = 0; k < mine; k++) {
+        const AdamwItem after = item_at(k + 2);
+        const int whole = (int)(it.count / 256), blocks = (int)((it.count + 255) / 256);
+        for (int block = wave; block < blocks || block == wave; block += 4) {
+            const bool last = block + 4 >= blocks;
+            const AdamwItem& from = last ? next : it;
+            const int to = last ? wave : block + 4;
+            const bool fetch = (!last || k + 1 < mine) && to < (int)(from.count / 256);
+            if (turn == 0) {
+                if (fetch) load_block<BITS, G, true>(from, to, lane, in[1]);
+                if (block < whole) step_block<BITS, G, C, true>(it, block, lane, in[0], s);
+            } else {
+                if (fetch) load_block<BITS, G, true>(from, to, lane, in[0]);
+                if (block < whole) step_block<BITS, G, C, true>(it, block, lane, in[1], s);
+            }
+            turn ^= 1;
+            if (block >= whole && block < blocks) {
+                BlockIn<BITS, G> tail;
+                load_block<BITS, G, false>(it, block, lane, tail);
+                step_block<BITS, G, C, false>(it, block, lane, tail, s);
+            }
         }
+        it = next;
+        next = after;
+    }
+    if (root == groups) {
+        __hip_atomic_store(&plan->arrived[0].count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(step, (int32_t)t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
 }
 
 template <int BITS, typename G>
 static void launch_grad_type(int copy_type, dim3 grid, AdamwHeader* plan, int64_t items, int32_t* step, const AdamwCall& call, hipStream_t stream)
 {
-    if (copy_type == FP6_F16) hipLaunchKernelGGL((adamw_kernel<BITS, G, _Float16>), grid, dim3(256), 0, stream, plan, items, step, call);
-    else if (copy_type == FP6_BF16) hipLaunchKernelGGL((adamw_kernel<BITS, G, __bf16>), grid, dim3(256), 0, stream, plan, items, step, call);
-    else hipLaunchKernelGGL((adamw_kernel<BITS, G, float>), grid, dim3(256), 0, stream, plan, items, step, call);
+    if (copy_type == FP6_F16) hipLaunchKernelGGL((adamw_kernel<BITS, G, _Float16>), grid, dim3(256), 0, stream, plan, (const AdamwItem*)(plan + 1), items, step, call);
+    else if (copy_type == FP6_BF16) hipLaunchKernelGGL((adamw_kernel<BITS, G, __bf16>), grid, dim3(256), 0, stream, plan, (const AdamwItem*)(plan + 1), items, step, call);
+    else hipLaunchKernelGGL((adamw_kernel<BITS, G, float>), grid, dim3(256), 0, stream, plan, (const AdamwItem*)(plan + 1), items, step, call);
 }
 
 template <int BITS>

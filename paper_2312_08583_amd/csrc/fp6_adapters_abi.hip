@@ -118,26 +118,24 @@ static size_t grad_inner(int format, int64_t M, int64_t N, int64_t K)
 
 static bool is_number(double v, double lo, double hi) { return v >= lo && v < hi; }
 
-static int64_t items_of(int64_t count) { return (count + kAdamwItem - 1) / kAdamwItem; }
-
 struct PlanLayout {
-    size_t blocks_at, items_at, bytes;
-    int64_t items;
+    int64_t item, items;
+    size_t bytes;
 };
 
 static bool plan_layout(const fp6_adamw_tensor* t, int64_t count, PlanLayout* l)
 {
     if (!t || count < 1 || count > (int64_t)1 << 24) return false;
-    int64_t items = 0;
+    int64_t elements = 0;
     for (int64_t i = 0; i < count; i++) {
         if (t[i].count < 0 || t[i].count > (int64_t)1 << 40) return false;
-        items += items_of(t[i].count);
-        if (items > (int64_t)1 << 31) return false;
+        elements += t[i].count;
+        if (elements > (int64_t)1 << 41) return false;
     }
-    l->items = items;
-    l->blocks_at = sizeof(AdamwHeader) + (size_t)count * sizeof(fp6_adamw_tensor);
-    l->items_at = (l->blocks_at + (size_t)count * 4 + 15) / 16 * 16;
-    l->bytes = l->items_at + (size_t)items * sizeof(AdamwItem);
+    l->item = adamw_item(elements);
+    l->items = 0;
+    for (int64_t i = 0; i < count; i++) l->items += (t[i].count + l->item - 1) / l->item;
+    l->bytes = sizeof(AdamwHeader) + (size_t)l->items * sizeof(AdamwItem);
     return true;
 }
 
@@ -190,25 +188,28 @@ static int adamw_plan(const fp6_adamw_tensor* t, int64_t count, int state_bits, 
         end_any = std::max(end_any, r.end);
         if (r.written) end_written = std::max(end_written, r.end);
     }
-    unsigned char* out = (unsigned char*)plan_host;
+    unsigned char* at = (unsigned char*)plan_host;
     AdamwHeader h{};
     h.magic = kAdamwMagic;
-    h.tensors = (uint32_t)count;
     h.state_bits = (uint32_t)state_bits;
-    h.blocks_at = l.blocks_at;
-    h.items_at = l.items_at;
     h.items = (uint64_t)l.items;
-    std::memcpy(out, &h, sizeof h);
-    std::memcpy(out + sizeof h, t, (size_t)count * sizeof *t);
-    uint32_t block = 0;
-    size_t at = l.items_at;
+    std::memcpy(at, &h, sizeof h);
+    at += sizeof h;
+    const int64_t grad_bytes = grad_type == FP6_F32 ? 4 : 2, state = state_bits == 8 ? 1 : 4;
+    uint32_t id = 0;                     // (numbers of elements wrap at 2^32: they only feed a hash)
     for (int64_t i = 0; i < count; i++) {
-        std::memcpy(out + l.blocks_at + 4 * (size_t)i, &block, 4);
-        block += (uint32_t)((t[i].count + 255) / 256);          // (numbers of elements wrap at 2^32: they only feed a hash)
-        for (int64_t p = 0; p < items_of(t[i].count); p++, at += sizeof(AdamwItem)) {
-            const AdamwItem item{(uint32_t)i, (uint32_t)p};
-            std::memcpy(out + at, &item, sizeof item);
+        const fp6_adamw_tensor& x = t[i];
+        for (int64_t e = 0; e < x.count; e += l.item, at += sizeof(AdamwItem)) {
+            AdamwItem item{x.param + e, (const char*)x.grad + grad_bytes * e, (char*)x.first + state * e, (char*)x.second + state * e,
+                           nullptr, nullptr, nullptr, id + (uint32_t)e, (uint32_t)std::min(l.item, x.count - e)};
+            if (state_bits == 8) {
+                item.first_scales = x.first_scales + e / 256;
+                item.second_scales = x.second_scales + e / 256;
+            }
+            if (copy_type != FP6_NO_COPY) item.copy = x.copy + e;
+            std::memcpy(at, &item, sizeof item);
         }
+        id += (uint32_t)((x.count + 255) / 256) * 256u;
     }
     *items = l.items;
     return FP6_OK;
