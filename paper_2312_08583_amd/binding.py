@@ -121,12 +121,15 @@ def _not_loaded(*_):
 # Marshalling in native code (csrc/fp6_python.cpp): the result of a plain call with its workspace, or None, and then the routines below
 # take the call: the checks are the same, allocations and errors are theirs.  Without the module they take every call.
 _native_linear = _native_group = _not_loaded
+_NATIVE_ADAPTERS = ("lora", "lora_group", "lora_backward", "linear_grad", "adamw")
+_native = dict.fromkeys(_NATIVE_ADAPTERS, _not_loaded)
 _LINEAR, _VARIANT, _FGQ, _FP5, _V2, _V2_BF16 = range(6)
 
 
 def _bind_native(L: ctypes.CDLL, path: str) -> None:
     global _native_linear, _native_group
     _native_linear = _native_group = _not_loaded
+    _native.update(dict.fromkeys(_NATIVE_ADAPTERS, _not_loaded))
     entries = (L.fp6_linear, L.fp6_linear_variant, L.fp6_linear_fgq, L.fp5_linear, L.fp6_linear_v2, L.fp6_linear_v2_bf16,
                L.fp6_linear_group, L.fp6_linear_workspace_bytes, L.fp6_linear_variant_workspace_bytes,
                L.fp6_linear_fgq_workspace_bytes, L.fp5_linear_workspace_bytes, L.fp6_linear_v2_workspace_bytes,
@@ -136,7 +139,11 @@ def _bind_native(L: ctypes.CDLL, path: str) -> None:
         native = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(native)
         native.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in entries), _check)
+        native.bind_adapters(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.fp6_lora_group, L.fp6_lora_backward, L.fp6_linear_grad,
+                                                                                L.fp6_adamw)))
+        adapters = {name: getattr(native, name) for name in _NATIVE_ADAPTERS}
         _native_linear, _native_group = native.linear, native.group
+        _native.update(adapters)
     except (ImportError, AttributeError, TypeError) as e:          # not there, not of this build, or of another version of bind()
         warnings.warn("%s: hot-path calls are marshalled in Python, 3 to 6 us slower each (python -m paper_2312_08583_amd.build "
                       "builds the module)" % e, RuntimeWarning, stacklevel=3)
@@ -692,6 +699,9 @@ def fp6_lora(X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, Y: torch.Tensor,
 
     X [M,K], Y [M,N], A [adapters,rank,K], B [adapters,N,rank], all fp16 or all bf16; index int32 [M] (None: adapter 0; outside
     the adapters: none, the row of Y stays); scaling fp32 [adapters]; hidden fp32 [M,rank] receives X A^T."""
+    done = _native["lora"](X, A, B, Y, index, scaling, hidden, out, workspace)
+    if done is not None:
+        return done
     call = _Call(X, "X")
     a, b, L, rank, N, K = _adapters(call, X, A, B)
     M = X.shape[0]
@@ -715,6 +725,9 @@ def fp6_lora_group(layers, index: Optional[torch.Tensor] = None, scaling: Option
                    workspace: Optional[torch.Tensor] = None):
     """fp6_lora for up to FP6_GROUP_MAX projections [(X, A, B, Y), ...] of the same rows, whose adapters and scaling are common, in
     one call.  Returns the list of results (without `outs`: the Y themselves)."""
+    done = _native["lora_group"](layers, index, scaling, outs, workspace)
+    if done is not None:
+        return done
     if not 1 <= len(layers) <= FP6_GROUP_MAX:
         raise Fp6Error("a group holds 1 to %d projections" % FP6_GROUP_MAX)
     if outs is not None and len(outs) != len(layers):
@@ -748,6 +761,9 @@ def fp6_lora_backward(dY: torch.Tensor, X: torch.Tensor, hidden: torch.Tensor, A
                       out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """The gradients of fp6_lora: (dX + scaling dY B A, dA, dB); dX None: no gradient for X.  dA and dB are fp32 and are added to
     where `accumulate` is set; `out` may be dX and is dX where it is not given."""
+    done = _native["lora_backward"](dY, X, hidden, A, B, dX, index, scaling, dA, dB, accumulate, out, workspace)
+    if done is not None:
+        return done
     call = _Call(X, "X")
     a, b, L, rank, N, K = _adapters(call, X, A, B)
     M = X.shape[0]
@@ -791,6 +807,9 @@ def fp6_linear_grad(dY: torch.Tensor, hi_t: torch.Tensor, lo_t: torch.Tensor, sc
                     format: int = FP6_FORMAT_E3M2, out: Optional[torch.Tensor] = None,
                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dX[M,K] = dY[M,N] x dequant(planes): the gradient of the frozen layer by its input, from the planes of fp6_transpose_pack."""
+    done = _native["linear_grad"](dY, hi_t, lo_t, scales_t, ratio, N, K, format, out, workspace)
+    if done is not None:
+        return done
     call = _Call(dY, "dY")
     _shape_ok(N, K)
     dtype = torch.bfloat16 if format == FP6_FORMAT_E3M2_V2_BF16 else torch.float16
@@ -860,6 +879,9 @@ def fp6_adamw(plan: AdamWPlan, step: torch.Tensor, lr=1e-3, beta1: float = 0.9, 
               seed: int = 0) -> None:
     """One AdamW step over the tensors of the plan, in place.  step: int32 [1], the steps done so far, counted on by the call; lr: a
     number, or fp32 [1] on the device; grad_scale fp32 [1] multiplies the gradients; found_inf fp32 [1]: not 0, and nothing changes."""
+    if _native["adamw"](plan.table, plan.items, plan.state_bits, plan.grad_type, plan.copy_type, step, lr, beta1, beta2, eps, weight_decay,
+                        grad_scale, found_inf, seed):
+        return
     call = _Call(plan.table, "plan")
     on_device = isinstance(lr, torch.Tensor)
     options = AdamWOptions(0.0 if on_device else float(lr), beta1, beta2, eps, weight_decay,

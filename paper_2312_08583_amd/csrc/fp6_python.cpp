@@ -1,4 +1,4 @@
-// Marshalling of the hot-path calls for Python: the same checks as binding.py makes, on the tensors themselves.
+// Marshalling of the hot-path calls for Python, and of those around the frozen layer: the same checks as binding.py makes, on the tensors themselves.
 //
 // A call from Python took 10 us, of which the kernel of a small layer is 3: some thirty attribute reads and checks, a ctypes call with
 // eleven conversions and the look-up of the current stream.  With them here it takes 3.3 to 4.4, most of it the launch (1 x 1024 x 1024,
@@ -12,6 +12,8 @@
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <initializer_list>
 
 #include "../../include/fp6_linear.h"
 
@@ -239,8 +241,311 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count)
     Py_RETURN_NONE;
 }
 
+// ---- the operators around the frozen layer
+
+decltype(&fp6_lora_group) call_lora_group;
+decltype(&fp6_lora_backward) call_lora_backward;
+decltype(&fp6_linear_grad) call_linear_grad;
+decltype(&fp6_adamw) call_adamw;
+
+// Checks of a call one after another; `ok` says whether all held.  Every tensor is a plain one on the current device.
+struct Checked {
+    bool ok = true;
+    c10::DeviceIndex device = -1;
+
+    const at::Tensor* tensor(PyObject* o, c10::ScalarType type)
+    {
+        const at::Tensor* t = ok ? plain(o, type) : nullptr;
+        if (!t || (device >= 0 && t->device().index() != device)) {
+            ok = false;
+            return nullptr;
+        }
+        if (device < 0) {
+            device = t->device().index();
+            if (device != c10::hip::getCurrentHIPStream().device_index()) ok = false;
+        }
+        return t;
+    }
+    void* sized(PyObject* o, c10::ScalarType type, std::initializer_list<int64_t> sizes)
+    {
+        const at::Tensor* t = tensor(o, type);
+        if (!t || t->dim() != (int64_t)sizes.size()) {
+            ok = false;
+            return nullptr;
+        }
+        int64_t d = 0;
+        for (const int64_t n : sizes) ok = ok && t->size(d++) == n;
+        return t->data_ptr();
+    }
+    void* flat(PyObject* o, c10::ScalarType type, int64_t count)
+    {
+        const at::Tensor* t = tensor(o, type);
+        if (t && t->numel() != count) ok = false;
+        return t ? t->data_ptr() : nullptr;
+    }
+    void* optional(PyObject* o, c10::ScalarType type, std::initializer_list<int64_t> sizes)
+    {
+        return o == Py_None ? nullptr : sized(o, type, sizes);
+    }
+};
+
+struct Adapters {
+    const void *x, *a, *b;
+    int64_t M, N, K, rank, adapters;
+    c10::ScalarType type;
+};
+
+// X [M,K], A [adapters, rank, K] and B [adapters, N, rank]
+bool read_adapters(Checked& c, PyObject* X, PyObject* A, PyObject* B, Adapters* r)
+{
+    if (!THPVariable_CheckExact(X)) return false;
+    const c10::ScalarType type = THPVariable_Unpack(X).scalar_type();
+    if (type != c10::kHalf && type != c10::kBFloat16) return false;
+    const at::Tensor *x = c.tensor(X, type), *a = c.tensor(A, type), *b = c.tensor(B, type);
+    if (!c.ok || x->dim() != 2 || a->dim() != 3 || b->dim() != 3 || x->size(0) < 1 || x->size(1) != a->size(2) || b->size(0) != a->size(0) ||
+        b->size(2) != a->size(1))
+        return false;
+    *r = Adapters{x->data_ptr(), a->data_ptr(), b->data_ptr(), x->size(0), b->size(1), x->size(1), a->size(1), a->size(0), type};
+    return true;
+}
+
+bool read_workspace(Checked& c, PyObject* o, void** p, size_t* bytes)
+{
+    const at::Tensor* t = c.tensor(o, c10::kByte);
+    if (!c.ok) return false;
+    *p = t->data_ptr();
+    *bytes = (size_t)t->numel();
+    return true;
+}
+
+int type_of(c10::ScalarType t) { return t == c10::kBFloat16 ? FP6_BF16 : FP6_F16; }
+
+// One projection of lora() and lora_group(): into `out`, or into Y where that is None.
+bool read_projection(Checked& c, PyObject* X, PyObject* A, PyObject* B, PyObject* Y, PyObject* out, PyObject* hidden, Adapters* r,
+                     fp6_lora_problem* p)
+{
+    if (!read_adapters(c, X, A, B, r)) return false;
+    void* y = c.sized(Y, r->type, {r->M, r->N});
+    void* o = out == Py_None ? y : c.sized(out, r->type, {r->M, r->N});
+    void* h = c.optional(hidden, c10::kFloat, {r->M, r->rank});
+    *p = fp6_lora_problem{(const uint16_t*)r->x, (const uint16_t*)r->a, (const uint16_t*)r->b, (const uint16_t*)y, (uint16_t*)o, (float*)h,
+                          r->N, r->K, r->rank};
+    return c.ok;
+}
+
+// lora(X, A, B, Y, index, scaling, hidden, out, workspace) -> out, or None
+PyObject* lora(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    if (count != 9 || !fail || modes_active()) Py_RETURN_NONE;
+    PyObject* result = a[7] == Py_None ? a[3] : a[7];
+    int status = FP6_OK;
+    try {
+        Checked c;
+        Adapters r;
+        fp6_lora_problem p;
+        void* ws;
+        size_t bytes;
+        if (!read_projection(c, a[0], a[1], a[2], a[3], a[7], a[6], &r, &p)) Py_RETURN_NONE;
+        const int32_t* index = (const int32_t*)c.optional(a[4], c10::kInt, {r.M});
+        const float* scaling = (const float*)c.optional(a[5], c10::kFloat, {r.adapters});
+        if (!read_workspace(c, a[8], &ws, &bytes)) Py_RETURN_NONE;
+        void* stream = c10::hip::getCurrentHIPStream().stream();
+        Py_INCREF(result);
+        Py_BEGIN_ALLOW_THREADS
+        status = call_lora_group(type_of(r.type), r.M, &p, 1, r.adapters, index, scaling, ws, bytes, stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    if (status == FP6_OK) return result;
+    Py_DECREF(result);
+    return PyObject_CallFunction(fail, "is", status, "fp6_lora");
+}
+
+// lora_group(layers, index, scaling, outs or None, workspace) -> list of results, or None
+PyObject* lora_group(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    if (count != 5 || !fail || modes_active()) Py_RETURN_NONE;
+    auto sequence = [](PyObject* o) { return PyList_CheckExact(o) || PyTuple_CheckExact(o); };
+    if (!sequence(a[0]) || (a[3] != Py_None && !sequence(a[3]))) Py_RETURN_NONE;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(a[0]);
+    if (n < 1 || n > FP6_GROUP_MAX || (a[3] != Py_None && PySequence_Fast_GET_SIZE(a[3]) != n)) Py_RETURN_NONE;
+    fp6_lora_problem problems[FP6_GROUP_MAX];
+    PyObject* results[FP6_GROUP_MAX];
+    int status = FP6_OK;
+    try {
+        Checked c;
+        Adapters first{}, r;
+        void* ws;
+        size_t bytes;
+        for (Py_ssize_t i = 0; i < n; i++) {
+            PyObject* l = PySequence_Fast_GET_ITEM(a[0], i);
+            PyObject* out = a[3] == Py_None ? Py_None : PySequence_Fast_GET_ITEM(a[3], i);
+            if (!sequence(l) || PySequence_Fast_GET_SIZE(l) != 4) Py_RETURN_NONE;
+            PyObject** f = PySequence_Fast_ITEMS(l);
+            if (!read_projection(c, f[0], f[1], f[2], f[3], out, Py_None, &r, &problems[i])) Py_RETURN_NONE;
+            if (i == 0) first = r;
+            if (r.M != first.M || r.adapters != first.adapters || r.type != first.type) Py_RETURN_NONE;
+            results[i] = out == Py_None ? f[3] : out;
+        }
+        const int32_t* index = (const int32_t*)c.optional(a[1], c10::kInt, {first.M});
+        const float* scaling = (const float*)c.optional(a[2], c10::kFloat, {first.adapters});
+        if (!read_workspace(c, a[4], &ws, &bytes)) Py_RETURN_NONE;
+        void* stream = c10::hip::getCurrentHIPStream().stream();
+        for (Py_ssize_t i = 0; i < n; i++) Py_INCREF(results[i]);          // (the lists may change while other threads run)
+        Py_BEGIN_ALLOW_THREADS
+        status = call_lora_group(type_of(first.type), first.M, problems, (int)n, first.adapters, index, scaling, ws, bytes, stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    PyObject* list = status == FP6_OK ? PyList_New(n) : nullptr;
+    for (Py_ssize_t i = 0; i < n; i++) {
+        if (list) PyList_SET_ITEM(list, i, results[i]);
+        else Py_DECREF(results[i]);
+    }
+    if (status != FP6_OK) return PyObject_CallFunction(fail, "is", status, "fp6_lora_group");
+    return list;
+}
+
+// lora_backward(dY, X, hidden, A, B, dX or None, index, scaling, dA, dB, accumulate, out or None, workspace) -> (out, dA, dB), or None
+PyObject* lora_backward(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    if (count != 13 || !fail || modes_active() || (a[10] != Py_True && a[10] != Py_False) || (a[5] == Py_None && a[11] != Py_None))
+        Py_RETURN_NONE;
+    PyObject* result = a[11] == Py_None ? a[5] : a[11];
+    PyObject* tuple = nullptr;
+    int status = FP6_OK;
+    try {
+        Checked c;
+        Adapters r;
+        void* ws;
+        size_t bytes;
+        if (!read_adapters(c, a[1], a[3], a[4], &r)) Py_RETURN_NONE;
+        const void* dy = c.sized(a[0], r.type, {r.M, r.N});
+        const float* hidden = (const float*)c.sized(a[2], c10::kFloat, {r.M, r.rank});
+        const void* dx = c.optional(a[5], r.type, {r.M, r.K});
+        const int32_t* index = (const int32_t*)c.optional(a[6], c10::kInt, {r.M});
+        const float* scaling = (const float*)c.optional(a[7], c10::kFloat, {r.adapters});
+        float* da = (float*)c.sized(a[8], c10::kFloat, {r.adapters, r.rank, r.K});
+        float* db = (float*)c.sized(a[9], c10::kFloat, {r.adapters, r.N, r.rank});
+        void* out = c.optional(result, r.type, {r.M, r.K});
+        if (!read_workspace(c, a[12], &ws, &bytes)) Py_RETURN_NONE;
+        void* stream = c10::hip::getCurrentHIPStream().stream();
+        tuple = PyTuple_Pack(3, result, a[8], a[9]);
+        if (!tuple) return nullptr;
+        const int accumulate = a[10] == Py_True;
+        Py_BEGIN_ALLOW_THREADS
+        status = call_lora_backward(type_of(r.type), (const uint16_t*)dy, (const uint16_t*)r.x, hidden, r.M, (const uint16_t*)r.a,
+                                    (const uint16_t*)r.b, r.adapters, r.rank, index, scaling, (const uint16_t*)dx, (uint16_t*)out, da, db,
+                                    accumulate, r.N, r.K, ws, bytes, stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_XDECREF(tuple);
+        Py_RETURN_NONE;
+    }
+    if (status == FP6_OK) return tuple;
+    Py_DECREF(tuple);
+    return PyObject_CallFunction(fail, "is", status, "fp6_lora_backward");
+}
+
+// linear_grad(dY, hi_t, lo_t, scales_t, ratio, N, K, format, out, workspace) -> out, or None
+PyObject* linear_grad(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    int64_t N, K, format;
+    if (count != 10 || !fail || !whole(a[5], &N) || !whole(a[6], &K) || !whole(a[7], &format) || modes_active()) Py_RETURN_NONE;
+    if (N <= 0 || K <= 0 || N % FP6_TILE || K % FP6_TILE || N > (int64_t)1 << 30 || K > (int64_t)1 << 30 || format < FP6_FORMAT_E3M1 ||
+        format > FP6_FORMAT_E3M2_V2_BF16)
+        Py_RETURN_NONE;
+    int status = FP6_OK;
+    try {
+        Checked c;
+        void* ws;
+        size_t bytes;
+        const c10::ScalarType type = format == FP6_FORMAT_E3M2_V2_BF16 ? c10::kBFloat16 : c10::kHalf;
+        const at::Tensor* dy = c.tensor(a[0], type);
+        if (!c.ok || dy->dim() != 2 || dy->size(1) != N || dy->size(0) < 1) Py_RETURN_NONE;
+        const int64_t M = dy->size(0);
+        const void *hi = c.flat(a[1], c10::kByte, N * K / 2), *lo = c.flat(a[2], c10::kByte, N * K / (format == FP6_FORMAT_E3M1 ? 8 : 4));
+        const uint16_t* scales = (const uint16_t*)c.flat(a[3], c10::kHalf, K);
+        const float* ratio = (const float*)c.flat(a[4], c10::kFloat, N);
+        uint16_t* out = (uint16_t*)c.sized(a[8], type, {M, K});
+        if (!read_workspace(c, a[9], &ws, &bytes)) Py_RETURN_NONE;
+        const uint16_t* from = (const uint16_t*)dy->data_ptr();
+        void* stream = c10::hip::getCurrentHIPStream().stream();
+        Py_INCREF(a[8]);
+        Py_BEGIN_ALLOW_THREADS
+        status = call_linear_grad((int)format, from, M, hi, lo, scales, ratio, N, K, out, ws, bytes, stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    if (status == FP6_OK) return a[8];
+    Py_DECREF(a[8]);
+    return PyObject_CallFunction(fail, "is", status, "fp6_linear_grad");
+}
+
+// adamw(table, items, state_bits, grad_type, copy_type, step, lr, beta1, beta2, eps, weight_decay, grad_scale, found_inf, seed) -> True, or None
+PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    int64_t items, bits, grad, copy, seed;
+    if (count != 14 || !fail || modes_active() || !whole(a[1], &items) || !whole(a[2], &bits) || !whole(a[3], &grad) || !whole(a[4], &copy) ||
+        !whole(a[13], &seed))
+        Py_RETURN_NONE;
+    for (int i = 7; i <= 10; i++)
+        if (!PyFloat_CheckExact(a[i])) Py_RETURN_NONE;
+    int status = FP6_OK;
+    try {
+        Checked c;
+        const at::Tensor* table = c.tensor(a[0], c10::kByte);
+        int32_t* step = (int32_t*)c.sized(a[5], c10::kInt, {1});
+        fp6_adamw_options o{};
+        if (PyFloat_CheckExact(a[6])) o.lr = PyFloat_AS_DOUBLE(a[6]);
+        else o.lr_device = (const float*)c.sized(a[6], c10::kFloat, {1});
+        o.beta1 = PyFloat_AS_DOUBLE(a[7]);
+        o.beta2 = PyFloat_AS_DOUBLE(a[8]);
+        o.eps = PyFloat_AS_DOUBLE(a[9]);
+        o.weight_decay = PyFloat_AS_DOUBLE(a[10]);
+        o.grad_scale = (const float*)c.optional(a[11], c10::kFloat, {1});
+        o.found_inf = (const float*)c.optional(a[12], c10::kFloat, {1});
+        o.seed = (uint32_t)seed;
+        if (!c.ok) Py_RETURN_NONE;
+        void* plan = table->data_ptr();
+        void* stream = c10::hip::getCurrentHIPStream().stream();
+        Py_BEGIN_ALLOW_THREADS
+        status = call_adamw(plan, items, (int)bits, (int)grad, (int)copy, step, &o, stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    if (status == FP6_OK) Py_RETURN_TRUE;
+    return PyObject_CallFunction(fail, "is", status, "fp6_adamw");
+}
+
+// bind_adapters(address of each entry point in the order of the declarations above); `fail` is bind()'s
+PyObject* bind_adapters(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    if (count != 4) return PyErr_Format(PyExc_TypeError, "bind_adapters takes four addresses");
+    void* p[4];
+    for (int i = 0; i < 4; i++) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    call_lora_group = (decltype(call_lora_group))p[0];
+    call_lora_backward = (decltype(call_lora_backward))p[1];
+    call_linear_grad = (decltype(call_linear_grad))p[2];
+    call_adamw = (decltype(call_adamw))p[3];
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {{"linear", (PyCFunction)(void (*)())linear, METH_FASTCALL, nullptr},
                          {"group", (PyCFunction)(void (*)())group, METH_FASTCALL, nullptr},
+                         {"lora", (PyCFunction)(void (*)())lora, METH_FASTCALL, nullptr},
+                         {"lora_group", (PyCFunction)(void (*)())lora_group, METH_FASTCALL, nullptr},
+                         {"lora_backward", (PyCFunction)(void (*)())lora_backward, METH_FASTCALL, nullptr},
+                         {"linear_grad", (PyCFunction)(void (*)())linear_grad, METH_FASTCALL, nullptr},
+                         {"adamw", (PyCFunction)(void (*)())adamw, METH_FASTCALL, nullptr},
+                         {"bind_adapters", (PyCFunction)(void (*)())bind_adapters, METH_FASTCALL, nullptr},
                          {"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -78,3 +78,13 @@ def test_a_module_appears_whole_or_not_at_all(monkeypatch, tmp_path):
     assert [p.read_bytes() for p in tmp_path.iterdir()] == [b"the one before"]
     hip_build.build_native()
     assert [p.read_bytes() for p in tmp_path.iterdir()] == [b"half and half"]
+
+
+def test_calls_around_the_layer_fall_back_with_the_module(fresh, tmp_path):
+    fresh.setattr(hip_build, "native_path", lambda: str(tmp_path / "none.so"))
+    with pytest.warns(RuntimeWarning, match="marshalled in Python"):
+        B.lib()
+    assert all(B._native[name] is B._not_loaded for name in B._NATIVE_ADAPTERS)
+    fresh.undo()
+    B._bind_native(B.lib(), hip_build.native_path())
+    assert not any(B._native[name] is B._not_loaded for name in B._NATIVE_ADAPTERS)
