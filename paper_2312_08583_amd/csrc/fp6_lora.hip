@@ -77,6 +77,13 @@ __device__ __forceinline__ void own_lds_order()
     __builtin_amdgcn_wave_barrier();
 }
 
+// Loads above stay above: left to itself the compiler moves each one down to its first use, to hold fewer registers, and waits there.
+__device__ __forceinline__ void loads_are_issued()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // ------------------------------------------------------------------ shrink
 struct ShrinkLayer {
     const uint16_t* Q;      // [M, C]
@@ -95,16 +102,21 @@ struct ShrinkArgs {
     int adapters, slots;
 };
 
+// Wavefronts of a shrink workgroup: four where it takes 64 rows; with few rows as many as share a contraction that is then cut into fewer
+// slices (LDS holds their sums, and the staged pieces of a turned W).
+template <int JT, int RT>
+constexpr int kShrinkWaves = RT > 1 || JT == 8 ? 4 : 8;
 template <int JT, int RT, bool TURNED>
-constexpr int kShrinkLds = TURNED && 4 * 64 * (16 * JT + 8) * 2 > 4 * RT * JT * 1024 ? 4 * 64 * (16 * JT + 8) * 2 : 4 * RT * JT * 1024;
+constexpr int kShrinkLds = kShrinkWaves<JT, RT> * (TURNED && 64 * (16 * JT + 8) * 2 > RT * JT * 1024 ? 64 * (16 * JT + 8) * 2 : RT * JT * 1024);
 
 // P[slice][m][j] = sum over the slice's c of Q[m][c] W[a][j][c].  A workgroup: 16 * RT rows, one slice of the contraction, whose
-// 64-wide units its four wavefronts take in turn; a lane holds 16 consecutive values of a row per unit (whole lines).  The
+// 64-wide units its wavefronts take in turn; four lanes share a row, and a load of theirs is 64 consecutive bytes of it.  The
 // distinct adapters of the rows are taken one after another, or one per grid slot: each reads its own A.
 template <int FMT, int JT, int RT, bool TURNED>
 __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, int slot, unsigned char* shared)
 {
     constexpr int kLd = 16 * JT + 8;                       // turned: elements between two rows of the staged unit
+    constexpr int WAVES = kShrinkWaves<JT, RT>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
     int which = 0;
@@ -121,14 +133,14 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
     const uint64_t none = RT == 4 ? ~pending : ~pending & (((uint64_t)1 << (16 * (RT & 3))) - 1);
     float* P = L.P + (size_t)slice * args.M * rank;
     if (slot == 0 && none) {                               // rows without an adapter
-        for (int e = threadIdx.x; e < 16 * RT * rank; e += 256)
+        for (int e = threadIdx.x; e < 16 * RT * rank; e += 64 * WAVES)
             if ((none >> (e / rank)) & 1 && m0 + e / rank < args.M) P[(size_t)(m0 + e / rank) * rank + e % rank] = 0.0f;
     }
     const uint16_t* q[RT];
 #pragma unroll
     for (int t = 0; t < RT; t++) {
         const int64_t row = min(m0 + 16 * t + i, args.M - 1);
-        q[t] = L.Q + (size_t)row * C + 16 * g;
+        q[t] = L.Q + (size_t)row * C + 8 * g;
     }
     // turned: the unit's 64 rows of W are one piece of memory, 2 * JT times 16 bytes a lane at most; where each goes in LDS
     uint16_t* own = reinterpret_cast<uint16_t*>(shared) + wave * (64 * kLd);
@@ -149,7 +161,7 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
         const uint16_t* W = L.W + (size_t)a * rank * C;
         const uint16_t* wj[JT];
 #pragma unroll
-        for (int j = 0; j < JT; j++) wj[j] = W + (size_t)min(16 * j + i, rank - 1) * C + 16 * g;
+        for (int j = 0; j < JT; j++) wj[j] = W + (size_t)min(16 * j + i, rank - 1) * C + 8 * g;
         float4v acc[RT][JT];
 #pragma unroll
         for (int t = 0; t < RT; t++)
@@ -162,12 +174,12 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
 #pragma unroll
             for (int t = 0; t < RT; t++)
 #pragma unroll
-                for (int h = 0; h < 2; h++) b.x[t][h] = *reinterpret_cast<const u32x4*>(q[t] + (size_t)u * 64 + 8 * h);
+                for (int h = 0; h < 2; h++) b.x[t][h] = *reinterpret_cast<const u32x4*>(q[t] + (size_t)u * 64 + 32 * h);
             if (!TURNED) {
 #pragma unroll
                 for (int j = 0; j < JT; j++)
 #pragma unroll
-                    for (int h = 0; h < 2; h++) b.w[j][h] = *reinterpret_cast<const u32x4*>(wj[j] + (size_t)u * 64 + 8 * h);
+                    for (int h = 0; h < 2; h++) b.w[j][h] = *reinterpret_cast<const u32x4*>(wj[j] + (size_t)u * 64 + 32 * h);
             } else {
                 const u32x4* piece = reinterpret_cast<const u32x4*>(W + (size_t)u * 64 * rank);
 #pragma unroll
@@ -190,7 +202,7 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
                     if (TURNED) {
 #pragma unroll
                         for (int e = 0; e < 2; e++) {
-                            const u32x2 d = read_turned(own + (16 * g + 8 * h + 4 * e + (i >> 2)) * kLd + min(16 * j + 4 * (i & 3), rank - 4));
+                            const u32x2 d = read_turned(own + (32 * h + 8 * g + 4 * e + (i >> 2)) * kLd + min(16 * j + 4 * (i & 3), rank - 4));
                             w[2 * e] = d[0];
                             w[2 * e + 1] = d[1];
                         }
@@ -203,17 +215,20 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
         if (u_begin < u_end) {
             // one unit in flight while another is used (past the end: the last one again, so that the loads need no branch)
             Unit b[2];
-            const int last = u_begin + (u_end - 1 - u_begin) / 4 * 4;
+            const int last = u_begin + (u_end - 1 - u_begin) / WAVES * WAVES;
             load(b[0], u_begin);
-            for (int u = u_begin; u < u_end; u += 8) {
-                if (RT > 1 || u + 4 < u_end) load(b[1], min(u + 4, last));
+            loads_are_issued();
+            for (int u = u_begin; u < u_end; u += 2 * WAVES) {
+                if (RT > 1 || u + WAVES < u_end) load(b[1], min(u + WAVES, last));
+                loads_are_issued();
                 compute(b[0]);
-                if (u + 4 >= u_end) break;
-                if (RT > 1 || u + 8 < u_end) load(b[0], min(u + 8, last));
+                if (u + WAVES >= u_end) break;
+                if (RT > 1 || u + 2 * WAVES < u_end) load(b[0], min(u + 2 * WAVES, last));
+                loads_are_issued();
                 compute(b[1]);
             }
         }
-        // the four wavefronts' sums meet in LDS, added in their order
+        // the wavefronts' sums meet in LDS, added in their order
         __syncthreads();
         float4v* meet = reinterpret_cast<float4v*>(shared);
 #pragma unroll
@@ -222,10 +237,10 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
             for (int j = 0; j < JT; j++) meet[(wave * RT * JT + t * JT + j) * 64 + lane] = acc[t][j];
         __syncthreads();
         const float s = args.scaling ? args.scaling[a] : 1.0f;
-        for (int tile = wave; tile < RT * JT; tile += 4) {
+        for (int tile = wave; tile < RT * JT; tile += WAVES) {
             float4v v = meet[tile * 64 + lane];
 #pragma unroll
-            for (int k = 1; k < 4; k++) v += meet[(k * RT * JT + tile) * 64 + lane];
+            for (int k = 1; k < WAVES; k++) v += meet[(k * RT * JT + tile) * 64 + lane];
             const int t = tile / JT, j = 16 * (tile % JT) + i;
 #pragma unroll
             for (int r = 0; r < 4; r++) {
@@ -238,7 +253,7 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
 }
 
 template <int FMT, int JT, int RT, bool TURNED>
-__global__ __launch_bounds__(256) void lora_shrink_kernel(ShrinkArgs args)
+__global__ __launch_bounds__((64 * kShrinkWaves<JT, RT>)) void lora_shrink_kernel(ShrinkArgs args)
 {
     __shared__ __align__(16) unsigned char shared[kShrinkLds<JT, RT, TURNED>];
     shrink_block<FMT, JT, RT, TURNED>(args, blockIdx.x, blockIdx.y, shared);
@@ -252,6 +267,8 @@ struct FinishArgs {
     float* power;            // [M]: 2^exponent
     int64_t M;
     int rank, slices, lanes; // lanes that share a row (a power of two, at least rank / 4)
+    const int32_t* index;    // rows without an adapter, which P may hold nothing for, are zeros
+    int adapters;
 };
 
 // The slices of the contraction added up, in their order, and split into the two terms that the expand kernel multiplies with: once a row
@@ -262,13 +279,14 @@ __global__ __launch_bounds__(256) void lora_finish_kernel(FinishArgs args)
     const int lanes = args.lanes, rank = args.rank;
     const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
     const int j = 4 * (int)(threadIdx.x % lanes);
-    const bool real = row < args.M && j < rank;
+    const bool real = row < args.M && j < rank, owned = real && adapter_of(args.index, row, args.M, args.adapters) != kNoAdapter;
     float4v v = float4v{0, 0, 0, 0};
     if (real) {
         const float* p = args.P + (size_t)row * rank + j;
         const size_t step = (size_t)args.M * rank;
 #pragma unroll 8
         for (int c = 0; c < args.slices; c++) v += *reinterpret_cast<const float4v*>(p + c * step);
+        if (!owned) v = float4v{0, 0, 0, 0};
         if (args.sum) *reinterpret_cast<float4v*>(args.sum + (size_t)row * rank + j) = v;
     }
     int exponent = 0;
@@ -290,6 +308,8 @@ __global__ __launch_bounds__(256) void lora_finish_kernel(FinishArgs args)
 }
 
 // ------------------------------------------------------------------ expand
+constexpr int kFewSlices = 8;            // slices at most that the expand kernel adds up itself
+
 struct ExpandLayer {
     const float* P;         // SLICED: [slices, M, rank]; else the power of two of each row
     const uint16_t* terms;  // else: [M][2][rank]
@@ -314,7 +334,8 @@ constexpr int kExpandLd = 64 + 8;        // turned: elements between two rows of
 template <bool TURNED>
 constexpr int kExpandLds = TURNED ? 4 * 32 * kExpandLd * 2 : 16;
 
-// out[m][n] = Y[m][n] + s * sum_j P[m][j] W[n][j].  A wavefront: 64 * CB columns n, 16 rows at a time; the lane of row l % 16 holds two
+// out[m][n] = Y[m][n] + s * sum_j P[m][j] W[n][j].  A wavefront: 64 * CB columns n, 16 rows at a time (the four of a workgroup side by side with
+// few rows, else one below the other, so that one of them brings W into the cache for all); the lane of row l % 16 holds two
 // pieces of eight consecutive columns of each 64 (the rows of the W operand are dealt out so that it does).  P is two 16-bit terms
 // times a power of two per row.  PACKED (rank <= 16): both terms share one MFMA of contraction 32.  W stays in registers from row
 // tile to row tile as long as the adapter is the same.  SLICED (few rows): the terms are made here from the slices.
@@ -326,11 +347,12 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
     int which = 0;
     while (which + 1 < args.layers && block >= args.layer[which + 1].first) which++;
     const ExpandLayer L = args.layer[which];
-    const int rank = L.rank, D = L.D, per_block = 256 * CB, blocks = (D + per_block - 1) / per_block, at = block - L.first;
-    const int n0 = (at % blocks) * per_block + wave * (64 * CB);
-    if (n0 >= D) return;
-    const int64_t tile0 = (int64_t)(at / blocks) * args.row_tiles;
+    constexpr int kAcross = (SLICED ? 4 : 1) * 64 * CB;          // columns of a workgroup
+    const int rank = L.rank, D = L.D, blocks = (D + kAcross - 1) / kAcross, at = block - L.first;
+    const int n0 = (at % blocks) * kAcross + (SLICED ? wave * (64 * CB) : 0);
+    const int64_t tile0 = ((int64_t)(at / blocks) * (SLICED ? 1 : 4) + (SLICED ? 0 : wave)) * args.row_tiles;
     const int64_t tiles = min((int64_t)args.row_tiles, (args.M + 15) / 16 - tile0);
+    if (n0 >= D || tiles <= 0) return;
     constexpr int TERMS = PACKED ? 1 : 2;
 
     struct Rows {                        // what a row tile needs: Y, the owner, and P where it is ready
@@ -422,34 +444,41 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
             const int a = __builtin_amdgcn_readlane(b.mine, __builtin_ctzll(pending));
             pending &= ~(__ballot(b.mine == a) & 0xFFFF);
             if (seen % args.slots != slot) continue;
-            if (a != held) hold(a);
             if (SLICED) {
-                // P of this lane's row: eight values per step
+                // P of this lane's row, eight values per step: the slices are asked for together, and W behind them
                 float v[JS][8];
                 float top = 0.0f;
 #pragma unroll
                 for (int s = 0; s < JS; s++) {
                     const int k0 = 32 * s + 8 * g, j0 = PACKED && k0 >= rank ? k0 - rank : k0;
-                    float4v lo = float4v{0, 0, 0, 0}, hi = lo;
-                    if (b.mine == a && j0 < rank) {
-                        const float* p = L.P + (size_t)row * rank + j0;
-                        const size_t step = (size_t)args.M * rank;
-#pragma unroll 8
-                        for (int c = 0; c < L.slices; c++) {
-                            lo += *reinterpret_cast<const float4v*>(p + c * step);
-                            hi += *reinterpret_cast<const float4v*>(p + c * step + 4);
+                    const bool real = b.mine == a && j0 < rank;
+                    const float* p = L.P + (size_t)min(row, args.M - 1) * rank + min(j0, rank - 8);
+                    const size_t step = (size_t)args.M * rank;
+                    float4v lo[kFewSlices], hi[kFewSlices];
+#pragma unroll
+                    for (int c = 0; c < kFewSlices; c++)
+                        if (c < L.slices) {
+                            lo[c] = *reinterpret_cast<const float4v*>(p + c * step);
+                            hi[c] = *reinterpret_cast<const float4v*>(p + c * step + 4);
                         }
-                        if (L.hidden && n0 == 0 && j0 == k0) {
-                            float4v* h = reinterpret_cast<float4v*>(L.hidden + (size_t)row * rank + j0);
-                            h[0] = lo;
-                            h[1] = hi;
+                    if (s == 0 && a != held) hold(a);
+                    loads_are_issued();
+#pragma unroll
+                    for (int c = 1; c < kFewSlices; c++)
+                        if (c < L.slices) {
+                            lo[0] += lo[c];
+                            hi[0] += hi[c];
                         }
+                    if (real && L.hidden && n0 == 0 && j0 == k0) {
+                        float4v* h = reinterpret_cast<float4v*>(L.hidden + (size_t)row * rank + j0);
+                        h[0] = lo[0];
+                        h[1] = hi[0];
                     }
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
-                        v[s][e] = lo[e];
-                        v[s][4 + e] = hi[e];
-                        top = fmaxf(top, fmaxf(fabsf(lo[e]), fabsf(hi[e])));
+                        v[s][e] = real ? lo[0][e] : 0.0f;
+                        v[s][4 + e] = real ? hi[0][e] : 0.0f;
+                        top = fmaxf(top, fmaxf(fabsf(v[s][e]), fabsf(v[s][4 + e])));
                     }
                 }
                 b.power = 1.0f;
@@ -482,6 +511,7 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
                     }
                 }
             }
+            if (!SLICED && a != held) hold(a);
             const float scale = args.scaling ? args.scaling[a] : 1.0f;
 #pragma unroll
             for (int c = 0; c < CB; c++) {
@@ -529,11 +559,14 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
         Rows b[2];
         load(b[0], 0);
         if (args.adapters == 1) hold(0);
+        loads_are_issued();
         for (int64_t t = 0; t < tiles; t += 2) {
             load(b[1], min(t + 1, tiles - 1));
+            loads_are_issued();
             work(b[0], t);
             if (t + 1 >= tiles) break;
             load(b[0], min(t + 2, tiles - 1));
+            loads_are_issued();
             work(b[1], t + 1);
         }
     }
@@ -555,17 +588,19 @@ struct OuterArgs {
     int C, rank, slices, adapters, splits, accumulate;
     const int32_t* index;
     const float* scaling;
+    const uint16_t* W;       // FUSED: [adapters, C, rank]
+    float* S;                // FUSED: [blocks of columns][M][rank]
 };
 
-constexpr int kChunk = 64;      // rows between two barriers
+constexpr int kChunk = 64;      // rows between two barriers (a lane of a wavefront each)
 
 template <int FMT, int JT, int CT>
 struct OuterLds {
     static constexpr int TERMS = FMT == kE3M2B ? 3 : 2, kCols = 64 * CT, kLdQ = kCols + 16, kLdP = kChunk + 8;
     uint16_t q[kChunk * kLdQ];
     uint16_t p[TERMS][16 * JT][kLdP];
-    uint32_t top[16 * JT];
-    float up[16 * JT];
+    uint32_t top[2][16 * JT];          // largest magnitudes of a chunk's columns of P, for this chunk and the next
+    uint64_t rows[kChunk];   // of 64 chunks: which rows are the adapter's
 };
 
 // G[a][j][c] = sum over the adapter's rows m of P[m][j] Q[m][c].  A workgroup: one adapter, 64 * CT columns, one range of rows, a
@@ -573,7 +608,9 @@ struct OuterLds {
 // turned, while the next chunk is on its way.  fp16: two terms, and a power of two per chunk and column of P, its products are added
 // up per chunk; bf16: three terms.  Rows of other adapters count as zeros on both sides (an infinity in one of them does not reach this
 // sum), chunks without a row of this one are passed over.
-template <int FMT, int JT, int CT, bool BY_COLUMN>
+// FUSED: the chunk of Q in LDS is multiplied with W as well, S[block][m][j] = s * sum over the block's columns of Q[m][c] W[a][c][j]: the part of
+// a shrink that this block of columns has, so that Q is read once for both.
+template <int FMT, int JT, int CT, bool BY_COLUMN, bool FUSED>
 __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, int a, OuterLds<FMT, JT, CT>& lds)
 {
     using Lds = OuterLds<FMT, JT, CT>;
@@ -605,47 +642,100 @@ __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, in
 #pragma unroll
         for (int c = 0; c < CT; c++) sum[j][c] = float4v{0, 0, 0, 0};
 
-    auto owner = [&](int chunk) { return adapter_of(args.index, (int64_t)chunk * kChunk + lane, args.M, args.adapters); };
-    int ahead = begin < end ? owner(begin) : kNoAdapter;          // of chunk `next`
-    int next = begin;
-    auto find = [&](uint64_t& rows) {                             // the next chunk with rows of this adapter, or end
-        while (next < end) {
-            const int chunk = next++;
-            rows = __ballot(ahead == a);
-            if (next < end) ahead = owner(next);
-            if (rows) return chunk;
+    // FUSED: W of the block's columns as operands, turned in LDS (each wavefront multiplies 16 rows with all columns)
+    constexpr int kSteps = FUSED ? kCols / 32 : 1, kLdW = 16 * JT + 8;
+    u32x4 w[FUSED ? JT : 1][kSteps];
+    if constexpr (FUSED) {
+        static_assert(kCols * kLdW <= kChunk * kLdQ, "W of the columns fits where the chunk of Q lies");
+        const int per = rank / 8, pieces = min(kCols, C - c0) * per;
+        const u32x4* from = reinterpret_cast<const u32x4*>(args.W + ((size_t)a * C + c0) * rank);
+        for (int p = threadIdx.x; p < kCols * per; p += 256)
+            *reinterpret_cast<u32x4*>(lds.q + (p / per) * kLdW + (p % per) * 8) = p < pieces ? from[p] : u32x4{0, 0, 0, 0};
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < JT; j++)
+#pragma unroll
+            for (int k = 0; k < kSteps; k++)
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const u32x2 d = read_turned(lds.q + (32 * k + 8 * g + 4 * e + (i >> 2)) * kLdW + min(16 * j + 4 * (i & 3), rank - 4));
+                    w[j][k][2 * e] = d[0];
+                    w[j][k][2 * e + 1] = d[1];
+                }
+    }
+    // The rows of this adapter, 64 chunks at a time: one load a lane and chunk, all under way together.
+    int batch = begin;
+    uint64_t todo = 0;               // chunks of the batch that have rows and are still to be done
+    auto gather = [&]() {
+        __syncthreads();
+        int owner[kChunk / 4];
+        auto row_of = [&](int v) { return (int64_t)(batch + wave + 4 * v) * kChunk + lane; };
+        if (args.index) {
+#pragma unroll
+            for (int v = 0; v < kChunk / 4; v++) owner[v] = args.index[min(row_of(v), args.M - 1)];
+            loads_are_issued();
+        } else {
+#pragma unroll
+            for (int v = 0; v < kChunk / 4; v++) owner[v] = 0;
         }
-        return end;
+#pragma unroll
+        for (int v = 0; v < kChunk / 4; v++) {
+            const uint64_t r = __ballot(owner[v] == a && batch + wave + 4 * v < end && row_of(v) < args.M);
+            if (lane == 0) lds.rows[wave + 4 * v] = r;
+        }
+        __syncthreads();
+        todo = __ballot(lds.rows[lane] != 0);
     };
+    auto find = [&](uint64_t& rows) {          // the next chunk with rows of this adapter, or end
+        while (!todo) {
+            batch += kChunk;
+            if (batch >= end) return end;
+            gather();
+        }
+        const int k = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        rows = lds.rows[k];
+        rows = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(rows >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)rows);
+        return batch + k;
+    };
+    // Loads take no branch: lanes of rows that are not the adapter's, and of columns past the end, read a row, or column, that is.  They count as
+    // zeros where the operands are put into LDS.
     u32x4 q[kQv];
     float4v p4[kPv];
     auto load = [&](int chunk, uint64_t rows) {
         const int64_t m0 = (int64_t)chunk * kChunk;
-        const uint16_t* from = args.Q + (size_t)m0 * C + c0 + qcol;
+        const int some = __builtin_ctzll(rows);
+        const uint16_t* from = args.Q + (size_t)m0 * C + (c0 + qcol < C ? c0 + qcol : c0);
 #pragma unroll
         for (int v = 0; v < kQv; v++) {
             const int row = qrow + kQstep * v;
-            q[v] = u32x4{0, 0, 0, 0};
-            if (((rows >> row) & 1) && c0 + qcol < C) q[v] = *reinterpret_cast<const u32x4*>(from + (size_t)row * C);
+            q[v] = *reinterpret_cast<const u32x4*>(from + (size_t)((rows >> row) & 1 ? row : some) * C);
         }
+        auto p_of = [&](int v) { return args.P + (size_t)(m0 + (prow[v] < kChunk && ((rows >> (prow[v] & 63)) & 1) ? prow[v] : some)) * rank + pj[v]; };
 #pragma unroll
-        for (int v = 0; v < kPv; v++) {
-            p4[v] = float4v{0, 0, 0, 0};
-            if (prow[v] < kChunk && ((rows >> prow[v]) & 1)) {
-                const float* at = args.P + (size_t)(m0 + prow[v]) * rank + pj[v];
-#pragma unroll 4
-                for (int c = 0; c < args.slices; c++) p4[v] += *reinterpret_cast<const float4v*>(at + (size_t)c * args.M * rank);
+        for (int v = 0; v < kPv; v++) p4[v] = *reinterpret_cast<const float4v*>(p_of(v));
+        if (args.slices > 1) {
+#pragma unroll
+            for (int v = 0; v < kPv; v++) {
+#pragma unroll 8
+                for (int c = 1; c < args.slices; c++) p4[v] += *reinterpret_cast<const float4v*>(p_of(v) + (size_t)c * args.M * rank);
             }
         }
     };
     uint64_t rows = 0;
-    int chunk = find(rows);
+    if (begin < end) gather();
+    int chunk = begin < end ? find(rows) : end;
     if (chunk < end) load(chunk, rows);
+    int turn = 0;
+    if (FMT != kE3M2B) {
+        if (threadIdx.x < 16 * JT) lds.top[0][threadIdx.x] = 0;
+        __syncthreads();
+    }
     while (chunk < end) {
-        __syncthreads();                                          // (the last chunk's operands have been read)
+#pragma unroll
+        for (int v = 0; v < kPv; v++)
+            if (!(prow[v] < kChunk && ((rows >> (prow[v] & 63)) & 1))) p4[v] = float4v{0, 0, 0, 0};
         if (FMT != kE3M2B) {
-            if (threadIdx.x < 16 * JT) lds.top[threadIdx.x] = 0;
-            __syncthreads();
 #pragma unroll
             for (int v = 0; v < kPv; v++) {
                 uint32_t m[4];                                    // (magnitudes order like their bits, NaN above all)
@@ -662,30 +752,63 @@ __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, in
                 }
                 if (prow[v] < kChunk && (!even || lane < per_row)) {
 #pragma unroll
-                    for (int e = 0; e < 4; e++) atomicMax(&lds.top[pj[v] + e], m[e]);
+                    for (int e = 0; e < 4; e++) atomicMax(&lds.top[turn][pj[v] + e], m[e]);
                 }
             }
-            __syncthreads();
-            if (threadIdx.x < 16 * JT) lds.up[threadIdx.x] = power_of_two(exponent_for(__builtin_bit_cast(float, lds.top[threadIdx.x])));
         }
+        if (rows != ~0ull || c0 + kCols > C) {
+#pragma unroll
+            for (int v = 0; v < kQv; v++)
+                if (!((rows >> (qrow + kQstep * v)) & 1) || c0 + qcol >= C) q[v] = u32x4{0, 0, 0, 0};
+        }
+        __syncthreads();                                          // (the largest are known, and the last chunk's operands have been read)
+        if (FMT != kE3M2B && threadIdx.x < 16 * JT) lds.top[turn ^ 1][threadIdx.x] = 0;
 #pragma unroll
         for (int v = 0; v < kQv; v++) *reinterpret_cast<u32x4*>(lds.q + (qrow + kQstep * v) * kLdQ + qcol) = q[v];
 #pragma unroll
         for (int v = 0; v < kPv; v++) {
-            if (prow[v] < kChunk)
+            if (prow[v] < kChunk) {
+                float down[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+                if (FMT != kE3M2B) {
+                    const u32x4 top = *reinterpret_cast<const u32x4*>(&lds.top[turn][pj[v]]);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const uint32_t t = top[e];
+                        down[e] = power_of_two(-exponent_for(__builtin_bit_cast(float, t)));
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     uint16_t t[TERMS];
-                    float x = p4[v][e];
-                    if (FMT != kE3M2B) x *= power_of_two(-exponent_for(__builtin_bit_cast(float, lds.top[pj[v] + e])));
-                    split_terms<FMT>(x, t);
+                    split_terms<FMT>(p4[v][e] * down[e], t);
 #pragma unroll
                     for (int k = 0; k < TERMS; k++) lds.p[k][pj[v] + e][prow[v]] = t[k];
                 }
+            }
         }
         __syncthreads();
+        const uint64_t these = rows;
+        const int64_t m0 = (int64_t)chunk * kChunk + 16 * wave + 4 * g;
         chunk = find(rows);
         if (chunk < end) load(chunk, rows);
+        loads_are_issued();
+        if (FUSED) {
+            float4v d[JT];
+#pragma unroll
+            for (int j = 0; j < JT; j++) d[j] = float4v{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < kSteps; k++) {
+                const half8 x = *reinterpret_cast<const half8*>(lds.q + (16 * wave + i) * kLdQ + 32 * k + 8 * g);
+#pragma unroll
+                for (int j = 0; j < JT; j++) d[j] = mfma16x16x32_of<FMT>(x, __builtin_bit_cast(half8, w[j][k]), d[j]);
+            }
+            float* S = args.S + ((size_t)(block % blocks) * args.M + m0) * rank;
+#pragma unroll
+            for (int j = 0; j < JT; j++)
+#pragma unroll
+                for (int r = 0; r < 4; r++)
+                    if (((these >> (16 * wave + 4 * g + r)) & 1) && 16 * j + i < rank) S[(size_t)r * rank + 16 * j + i] = d[j][r] * s;
+        }
         float4v part[JT][CT];
         float4v (&acc)[JT][CT] = FMT == kE3M2B ? sum : part;
         if (FMT != kE3M2B) {
@@ -719,11 +842,18 @@ __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, in
         if (FMT != kE3M2B) {
 #pragma unroll
             for (int j = 0; j < JT; j++) {
-                const float4v f = *reinterpret_cast<const float4v*>(lds.up + 16 * j + 4 * g);
+                const u32x4 top = *reinterpret_cast<const u32x4*>(&lds.top[turn][16 * j + 4 * g]);
+                float4v f;
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    const uint32_t t = top[r];
+                    f[r] = power_of_two(exponent_for(__builtin_bit_cast(float, t)));
+                }
 #pragma unroll
                 for (int c = 0; c < CT; c++) sum[j][c] += part[j][c] * f;
             }
         }
+        turn ^= 1;
     }
     float* G = args.G + ((size_t)split * args.adapters + a) * rank * C;
     const bool add = args.accumulate && args.splits == 1;
@@ -748,11 +878,11 @@ __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, in
         }
 }
 
-template <int FMT, int JT, int CT, bool BY_COLUMN>
+template <int FMT, int JT, int CT, bool BY_COLUMN, bool FUSED>
 __global__ __launch_bounds__(256) void lora_outer_kernel(OuterArgs args)
 {
     __shared__ __align__(16) OuterLds<FMT, JT, CT> lds;
-    outer_block<FMT, JT, CT, BY_COLUMN>(args, blockIdx.x, blockIdx.y, lds);
+    outer_block<FMT, JT, CT, BY_COLUMN, FUSED>(args, blockIdx.x, blockIdx.y, lds);
 }
 
 // out[k] (+)= the sum over the splits, in their order; two tensors in one launch
@@ -784,7 +914,7 @@ static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kFewRows = 64;
 
 // Rows a shrink workgroup takes, slots its adapters are dealt to, and slices of the contraction: two workgroups for each compute unit
-// where the contraction is long enough to be cut (a slice gives each of the four wavefronts at least one unit of 64).
+// (one, with few rows) where the contraction is long enough to be cut (a slice gives each wavefront at least one unit of 64).
 struct ShrinkPlan {
     int row_tiles, slots, slices;
     int64_t groups;
@@ -797,24 +927,45 @@ static ShrinkPlan plan_shrink(int64_t M, int C, int rank, int adapters)
     const int64_t rows = 16 * p.row_tiles;
     p.groups = ceil_div(M, rows);
     p.slots = M <= kFewRows ? (int)(adapters < rows ? adapters : rows) : 1;
-    const int64_t have = p.groups * p.slots, most = C / 64 >= 8 ? C / 256 : 1;
-    int64_t slices = ceil_div(512, have);
+    const int waves = M > kFewRows || rank > 64 ? 4 : 8, limit = M > kFewRows ? 16 : kFewSlices;
+    const int64_t have = p.groups * p.slots, most = C / (64 * waves);
+    int64_t slices = ceil_div(M > kFewRows ? 512 : 256, have);
     if (slices > most) slices = most;
-    if (slices > 16) slices = 16;
+    if (slices > limit) slices = limit;
     p.slices = (int)(slices < 1 ? 1 : slices);
     return p;
 }
 
-// Ranges of rows that separate workgroups of the outer products take: two workgroups for each compute unit, of at least four chunks.
-static int plan_splits(int64_t M, int C, int cols, int adapters)
+// Columns of an outer workgroup, and ranges of rows that separate workgroups take.  Two workgroups fit a compute unit, 512 are a round (516 took
+// 70 us where 430 take LATER_FUSED); a workgroup needs about 4 us beside its chunks and 3 (128 columns: 2.2) for each, adapters sharing
+// the rows evenly; every range costs a tensor of partial sums, written and read at 4 TB/s, and together they cost a launch.
+struct OuterPlan {
+    int columns, splits;
+};
+
+static OuterPlan plan_outer(int64_t M, int C, int rank, int adapters, bool fused)
 {
-    const int64_t chunks = ceil_div(M, kChunk), have = ceil_div(C, cols) * adapters;
-    int64_t splits = ceil_div(512, have);
-    if (splits > chunks / 4) splits = chunks / 4;
-    return (int)(splits < 1 ? 1 : (splits > 64 ? 64 : splits));
+    OuterPlan best{256, 1};
+    double least = 1e30;
+    const int64_t chunks = ceil_div(M, kChunk);
+    for (int columns = 256; columns >= 128; columns -= 128) {
+        if (columns == 256 ? rank > 64 : fused) continue;
+        const int64_t have = ceil_div(C, columns) * adapters;
+        for (int splits = 1; splits <= 64 && splits <= chunks; splits++) {
+            const double chunk = columns == 256 ? 3.0 : 2.2, mine = (double)ceil_div(chunks, (int64_t)splits * adapters);
+            const double partial = splits > 1 ? 4.0 + 8e-6 * splits * adapters * rank * C / 4 : 0.0;
+            const double cost = (double)ceil_div(have * splits, 512) * (4.0 + chunk * mine) + partial;
+            if (cost < least) {
+                least = cost;
+                best = OuterPlan{columns, splits};
+            }
+        }
+    }
+    return best;
 }
 
-static int outer_columns(int rank) { return rank > 64 ? 128 : 256; }
+// The gradient of B and the shrink of dY in one reading of dY: the shrink's parts, one per 256 columns, cost rank / 64 of what they save.
+static bool fuses(int64_t M, int rank) { return M > kFewRows && rank <= 32; }
 
 template <int FMT, bool TURNED>
 static hipError_t launch_shrink(const ShrinkArgs& a, bool few, int64_t workgroups, hipStream_t stream)
@@ -823,10 +974,10 @@ static hipError_t launch_shrink(const ShrinkArgs& a, bool few, int64_t workgroup
     for (int l = 0; l < a.layers; l++) rank = a.layer[l].rank > rank ? a.layer[l].rank : rank;
     const dim3 grid((unsigned)workgroups, (unsigned)a.slots), block(256);
     if (few) {
-        if (rank <= 16) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 1, TURNED>), grid, block, 0, stream, a);
-        else if (rank <= 32) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 1, TURNED>), grid, block, 0, stream, a);
-        else if (rank <= 64) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, 1, TURNED>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 8, 1, TURNED>), grid, block, 0, stream, a);
+        if (rank <= 16) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 1, TURNED>), grid, dim3(64 * kShrinkWaves<1, 1>), 0, stream, a);
+        else if (rank <= 32) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 1, TURNED>), grid, dim3(64 * kShrinkWaves<2, 1>), 0, stream, a);
+        else if (rank <= 64) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, 1, TURNED>), grid, dim3(64 * kShrinkWaves<4, 1>), 0, stream, a);
+        else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 8, 1, TURNED>), grid, dim3(64 * kShrinkWaves<8, 1>), 0, stream, a);
     } else {
         if (rank <= 16) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 4, TURNED>), grid, block, 0, stream, a);
         else if (rank <= 32) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 4, TURNED>), grid, block, 0, stream, a);
@@ -837,17 +988,18 @@ static hipError_t launch_shrink(const ShrinkArgs& a, bool few, int64_t workgroup
 }
 
 template <int FMT>
-static hipError_t launch_finish(const float* P, float* sum, uint16_t* terms, float* power, int64_t M, int rank, int slices, hipStream_t stream)
+static hipError_t launch_finish(const float* P, float* sum, uint16_t* terms, float* power, int64_t M, int rank, int slices, const int32_t* index,
+                                int adapters, hipStream_t stream)
 {
     int lanes = 2;
     while (4 * lanes < rank) lanes *= 2;
-    const FinishArgs f{P, sum, terms, power, M, rank, slices, lanes};
+    const FinishArgs f{P, sum, terms, power, M, rank, slices, lanes, index, adapters};
     hipLaunchKernelGGL(lora_finish_kernel<FMT>, dim3((unsigned)ceil_div(M * lanes, 256)), dim3(256), 0, stream, f);
     return hipGetLastError();
 }
 
-// 64-wide blocks of columns that a wavefront of the expand kernel takes side by side
-static int expand_blocks(bool few, int rank) { return few || rank > 64 ? 1 : 2; }
+// Columns of an expand workgroup
+static int expand_across(bool few, int rank) { return few ? 256 : (rank > 64 ? 64 : 128); }
 
 template <int FMT, bool TURNED>
 static hipError_t launch_expand(const ExpandArgs& a, bool few, int rank, int64_t workgroups, hipStream_t stream)
@@ -869,25 +1021,40 @@ static hipError_t launch_expand(const ExpandArgs& a, bool few, int rank, int64_t
     return hipGetLastError();
 }
 
-template <int FMT, bool BY_COLUMN>
-static hipError_t launch_outer(const OuterArgs& a, hipStream_t stream)
+template <int FMT, int CT, bool BY_COLUMN>
+static void launch_outer_rank(const OuterArgs& a, dim3 grid, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(ceil_div(a.C, outer_columns(a.rank)) * a.splits), (unsigned)a.adapters);
-    if (a.rank <= 16) hipLaunchKernelGGL((lora_outer_kernel<FMT, 1, 4, BY_COLUMN>), grid, dim3(256), 0, stream, a);
-    else if (a.rank <= 32) hipLaunchKernelGGL((lora_outer_kernel<FMT, 2, 4, BY_COLUMN>), grid, dim3(256), 0, stream, a);
-    else if (a.rank <= 64) hipLaunchKernelGGL((lora_outer_kernel<FMT, 4, 4, BY_COLUMN>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((lora_outer_kernel<FMT, 8, 2, BY_COLUMN>), grid, dim3(256), 0, stream, a);
+    if (a.rank <= 16) hipLaunchKernelGGL((lora_outer_kernel<FMT, 1, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
+    else if (a.rank <= 32) hipLaunchKernelGGL((lora_outer_kernel<FMT, 2, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
+    else if (a.rank <= 64) hipLaunchKernelGGL((lora_outer_kernel<FMT, 4, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((lora_outer_kernel<FMT, 8, 2, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
+}
+
+template <int FMT, bool BY_COLUMN>
+static hipError_t launch_outer(const OuterArgs& a, int columns, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(ceil_div(a.C, columns) * a.splits), (unsigned)a.adapters);
+    if (a.S) {
+        if (a.rank <= 16) hipLaunchKernelGGL((lora_outer_kernel<FMT, 1, 4, true, true>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((lora_outer_kernel<FMT, 2, 4, true, true>), grid, dim3(256), 0, stream, a);
+    } else if (columns == 128) {
+        launch_outer_rank<FMT, 2, BY_COLUMN>(a, grid, stream);
+    } else {
+        launch_outer_rank<FMT, 4, BY_COLUMN>(a, grid, stream);
+    }
     return hipGetLastError();
 }
 
-// Row tiles of 16 rows that an expand workgroup takes one after another (its operands of W stay in registers, and the next tile's loads are in
-// flight): as many as leave four workgroups for each compute unit, eight at most.
+// Row tiles of 16 rows that a wavefront of the expand kernel takes one after another (its operands of W stay in registers, and the next tile's loads
+// are in flight): as many as leave two workgroups for each compute unit, eight at most.
 static int expand_row_tiles(int64_t M, int64_t column_blocks)
 {
     if (M <= kFewRows) return 1;
-    const int64_t tiles = ceil_div(M, 16), t = tiles * column_blocks / 1024;
+    const int64_t tiles = ceil_div(M, 64), t = tiles * column_blocks / 512;
     return (int)(t < 1 ? 1 : (t > 8 ? 8 : t));
 }
+
+static int64_t expand_groups(int64_t M, bool few, int row_tiles) { return ceil_div(M, 16 * (few ? 1 : 4) * row_tiles); }
 
 static size_t round_up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -936,7 +1103,7 @@ static hipError_t launch_lora_t(int64_t M, const fp6_lora_problem* pr, int count
     e.scaling = scaling;
     s.adapters = e.adapters = adapters;
     const bool few = M <= kFewRows;
-    const int rank = group_rank(pr, count), across = 256 * expand_blocks(few, rank);
+    const int rank = group_rank(pr, count), across = expand_across(few, rank);
     unsigned char* at = workspace + kZeroBytes;
     int64_t shrinks = 0, expands = 0, columns = 0;
     for (int l = 0; l < count; l++) columns += ceil_div(pr[l].N, across);
@@ -950,12 +1117,12 @@ static hipError_t launch_lora_t(int64_t M, const fp6_lora_problem* pr, int count
                                  pr[l].B, pr[l].Y, pr[l].out, pr[l].hidden, (int)pr[l].N, (int)pr[l].rank, p.slices, (int)expands};
         at += space.bytes;
         shrinks += p.groups * p.slices;
-        expands += ceil_div(pr[l].N, across) * ceil_div(ceil_div(M, 16), e.row_tiles);
+        expands += ceil_div(pr[l].N, across) * expand_groups(M, few, e.row_tiles);
     }
     hipError_t err = launch_shrink<FMT, false>(s, few, shrinks, stream);
     for (int l = 0; l < count && !few && err == hipSuccess; l++)
         err = launch_finish<FMT>(s.layer[l].P, pr[l].hidden, const_cast<uint16_t*>(e.layer[l].terms), const_cast<float*>(e.layer[l].P), M,
-                                 (int)pr[l].rank, s.layer[l].slices, stream);
+                                 (int)pr[l].rank, s.layer[l].slices, index, adapters, stream);
     if (err != hipSuccess) return err;
     return launch_expand<FMT, false>(e, few, rank, expands, stream);
 }
@@ -972,19 +1139,22 @@ hipError_t launch_lora(bool bf16, int64_t M, const fp6_lora_problem* pr, int cou
 struct BackwardPlan {
     ShrinkPlan shrink;
     ShrinkSpace space;
-    int splits_a, splits_b;
+    OuterPlan a, b;
+    bool fused;
     size_t da, db;           // bytes
 };
 
 static BackwardPlan plan_backward(int64_t M, int64_t N, int64_t K, int rank, int adapters)
 {
     BackwardPlan p;
+    p.fused = fuses(M, rank);
+    p.a = plan_outer(M, (int)K, rank, adapters, false);
+    p.b = plan_outer(M, (int)N, rank, adapters, p.fused);
     p.shrink = plan_shrink(M, (int)N, rank, adapters);
+    if (p.fused) p.shrink.slices = (int)ceil_div(N, p.b.columns);
     p.space = shrink_space(p.shrink, M, rank);
-    p.splits_a = plan_splits(M, (int)K, outer_columns(rank), adapters);
-    p.splits_b = plan_splits(M, (int)N, outer_columns(rank), adapters);
-    p.da = p.splits_a > 1 ? round_up((size_t)p.splits_a * adapters * rank * K * 4) : 0;
-    p.db = p.splits_b > 1 ? round_up((size_t)p.splits_b * adapters * rank * N * 4) : 0;
+    p.da = p.a.splits > 1 ? round_up((size_t)p.a.splits * adapters * rank * K * 4) : 0;
+    p.db = p.b.splits > 1 ? round_up((size_t)p.b.splits * adapters * rank * N * 4) : 0;
     return p;
 }
 
@@ -1005,25 +1175,29 @@ static hipError_t launch_backward_t(const LoraBackward& b, unsigned char* worksp
     float* power = (float*)(at + p.space.slices + p.space.terms);
     float* da = (float*)(at + p.space.bytes);
     float* db = (float*)(at + p.space.bytes + p.da);
-    ShrinkArgs s{};
-    s.layers = 1;
-    s.M = b.M;
-    s.index = b.index;
-    s.scaling = b.scaling;
-    s.adapters = b.adapters;
-    s.slots = p.shrink.slots;
-    s.layer[0] = ShrinkLayer{b.dY, b.B, dh, (int)b.N, b.rank, p.shrink.slices, 0};
-    hipError_t err = launch_shrink<FMT, true>(s, few, p.shrink.groups * p.shrink.slices, stream);
-    if (err != hipSuccess) return err;
-    // (right behind the shrink: what the last-level cache still holds of dY is read from there)
-    const OuterArgs ob{b.hidden, b.dY, p.splits_b > 1 ? db : b.dB, b.M, (int)b.N, b.rank, 1, b.adapters, p.splits_b, b.accumulate, b.index, b.scaling};
-    err = launch_outer<FMT, true>(ob, stream);
+    hipError_t err = hipSuccess;
+    if (!p.fused) {
+        ShrinkArgs s{};
+        s.layers = 1;
+        s.M = b.M;
+        s.index = b.index;
+        s.scaling = b.scaling;
+        s.adapters = b.adapters;
+        s.slots = p.shrink.slots;
+        s.layer[0] = ShrinkLayer{b.dY, b.B, dh, (int)b.N, b.rank, p.shrink.slices, 0};
+        err = launch_shrink<FMT, true>(s, few, p.shrink.groups * p.shrink.slices, stream);
+        if (err != hipSuccess) return err;
+    }
+    // (right behind the shrink, where it is not part of it: what the last-level cache still holds of dY is read from there)
+    const OuterArgs ob{b.hidden, b.dY, p.b.splits > 1 ? db : b.dB, b.M, (int)b.N, b.rank, 1, b.adapters, p.b.splits, b.accumulate, b.index, b.scaling,
+                       p.fused ? b.B : nullptr, p.fused ? dh : nullptr};
+    err = launch_outer<FMT, true>(ob, p.b.columns, stream);
     if (err != hipSuccess) return err;
     // the sum over the slices goes where the first slice lies
-    if (!few) err = launch_finish<FMT>(dh, dh, terms, power, b.M, b.rank, p.shrink.slices, stream);
+    if (!few) err = launch_finish<FMT>(dh, dh, terms, power, b.M, b.rank, p.shrink.slices, b.index, b.adapters, stream);
     if (err != hipSuccess) return err;
     if (b.out) {
-        const int across = 256 * expand_blocks(few, b.rank);
+        const int across = expand_across(few, b.rank);
         ExpandArgs e{};
         e.layers = 1;
         e.M = b.M;
@@ -1032,22 +1206,23 @@ static hipError_t launch_backward_t(const LoraBackward& b, unsigned char* worksp
         e.slots = p.shrink.slots;
         e.row_tiles = expand_row_tiles(b.M, ceil_div(b.K, across));
         e.layer[0] = ExpandLayer{few ? dh : power, terms, b.A, b.dX, b.out, nullptr, (int)b.K, b.rank, p.shrink.slices, 0};
-        err = launch_expand<FMT, true>(e, few, b.rank, ceil_div(b.K, across) * ceil_div(ceil_div(b.M, 16), e.row_tiles), stream);
+        err = launch_expand<FMT, true>(e, few, b.rank, ceil_div(b.K, across) * expand_groups(b.M, few, e.row_tiles), stream);
         if (err != hipSuccess) return err;
     }
-    const OuterArgs oa{dh, b.X, p.splits_a > 1 ? da : b.dA, b.M, (int)b.K, b.rank, few ? p.shrink.slices : 1, b.adapters, p.splits_a, b.accumulate, b.index, nullptr};
-    err = launch_outer<FMT, false>(oa, stream);
-    if (err != hipSuccess || (p.splits_a == 1 && p.splits_b == 1)) return err;
+    const OuterArgs oa{dh, b.X, p.a.splits > 1 ? da : b.dA, b.M, (int)b.K, b.rank, few ? p.shrink.slices : 1, b.adapters, p.a.splits, b.accumulate,
+                       b.index, nullptr, nullptr, nullptr};
+    err = launch_outer<FMT, false>(oa, p.a.columns, stream);
+    if (err != hipSuccess || (p.a.splits == 1 && p.b.splits == 1)) return err;
     JoinArgs j{};
     j.accumulate = b.accumulate;
     j.part[0] = (const float4v*)da;
     j.out[0] = (float4v*)b.dA;
-    j.count[0] = p.splits_a > 1 ? (int64_t)b.adapters * b.rank * b.K / 4 : 0;
-    j.splits[0] = p.splits_a;
+    j.count[0] = p.a.splits > 1 ? (int64_t)b.adapters * b.rank * b.K / 4 : 0;
+    j.splits[0] = p.a.splits;
     j.part[1] = (const float4v*)db;
     j.out[1] = (float4v*)b.dB;
-    j.count[1] = p.splits_b > 1 ? (int64_t)b.adapters * b.rank * b.N / 4 : 0;
-    j.splits[1] = p.splits_b;
+    j.count[1] = p.b.splits > 1 ? (int64_t)b.adapters * b.rank * b.N / 4 : 0;
+    j.splits[1] = p.b.splits;
     const int64_t want = ceil_div(j.count[0] + j.count[1], 256);
     hipLaunchKernelGGL(lora_join_kernel, dim3((unsigned)(want < 4096 ? want : 4096)), dim3(256), 0, stream, j);
     return hipGetLastError();
