@@ -44,6 +44,10 @@ static int lora_numbers(int type, int64_t rank, int64_t adapters)
 
 // Workgroups of the launches are counted in 31 bits.
 static bool lora_fits(int64_t M, int64_t columns) { return (M + 15) / 16 * ((columns + 255) / 256) < (int64_t)1 << 28; }
+static bool backward_fits(int64_t M, int64_t N, int64_t K, int64_t adapters)
+{
+    return lora_fits(M, std::max(N, K)) && (std::max(N, K) + 127) / 128 * adapters < (int64_t)1 << 24;
+}
 
 static int lora_check(int type, int64_t M, const fp6_lora_problem* pr, int count, int64_t adapters)
 {
@@ -251,7 +255,7 @@ int fp6_lora(int type, const uint16_t* X, int64_t M, const uint16_t* A, const ui
 
 size_t fp6_lora_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t rank, int64_t adapters)
 {
-    if (!rows_ok(M) || !shape_ok(N, K) || lora_numbers(FP6_F16, rank, adapters) != FP6_OK || !lora_fits(M, std::max(N, K))) return 0;
+    if (!rows_ok(M) || !shape_ok(N, K) || lora_numbers(FP6_F16, rank, adapters) != FP6_OK || !backward_fits(M, N, K, adapters)) return 0;
     return lora_backward_workspace(M, N, K, (int)rank, (int)adapters);
 }
 
@@ -263,7 +267,7 @@ int fp6_lora_backward(int type, const uint16_t* dY, const uint16_t* X, const flo
     if (!dY || !X || !hidden || !A || !B || !dA || !dB || !dX != !out) return FP6_ERR_NULL;
     const int bad = lora_numbers(type, rank, adapters);
     if (bad != FP6_OK) return bad;
-    if (!rows_ok(M) || !shape_ok(N, K) || !lora_fits(M, std::max(N, K))) return FP6_ERR_SHAPE;
+    if (!rows_ok(M) || !shape_ok(N, K) || !backward_fits(M, N, K, adapters)) return FP6_ERR_SHAPE;
     const void* all[] = {dY, X, hidden, A, B, index, scaling, dX, out, dA, dB, workspace};
     for (const void* p : all)
         if (!aligned16(p)) return FP6_ERR_ALIGN;

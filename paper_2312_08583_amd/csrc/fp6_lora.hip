@@ -16,13 +16,18 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kNoAdapter = -1;
 
-// The adapter of a row, or kNoAdapter.
+// The adapter of a row, or kNoAdapter: what index holds for it (of the last row past the end: the load takes no branch), and whether that is one.
+__device__ __forceinline__ int owner_word(const int32_t* __restrict__ index, int64_t row, int64_t M)
+{
+    return index ? index[min(row, M - 1)] : 0;
+}
+__device__ __forceinline__ int owner_of(int word, int64_t row, int64_t M, int adapters)
+{
+    return row < M && (unsigned)word < (unsigned)adapters ? word : kNoAdapter;
+}
 __device__ __forceinline__ int adapter_of(const int32_t* __restrict__ index, int64_t row, int64_t M, int adapters)
 {
-    if (row >= M) return kNoAdapter;
-    if (!index) return 0;
-    const int a = index[row];
-    return (unsigned)a < (unsigned)adapters ? a : kNoAdapter;
+    return owner_of(owner_word(index, row, M), row, M, adapters);
 }
 
 template <int FMT>
@@ -106,17 +111,16 @@ struct ShrinkArgs {
 // slices (LDS holds their sums, and the staged pieces of a turned W).
 template <int JT, int RT>
 constexpr int kShrinkWaves = RT > 1 || JT == 8 ? 4 : 8;
-template <int JT, int RT, bool TURNED>
-constexpr int kShrinkLds = kShrinkWaves<JT, RT> * (TURNED && 64 * (16 * JT + 8) * 2 > RT * JT * 1024 ? 64 * (16 * JT + 8) * 2 : RT * JT * 1024);
+template <int JT, int RT, bool TURNED, int WAVES>
+constexpr int kShrinkLds = WAVES * (TURNED && 32 * (16 * JT + 8) * 2 > RT * JT * 1024 ? 32 * (16 * JT + 8) * 2 : RT * JT * 1024);
 
 // P[slice][m][j] = sum over the slice's c of Q[m][c] W[a][j][c].  A workgroup: 16 * RT rows, one slice of the contraction, whose
 // 64-wide units its wavefronts take in turn; four lanes share a row, and a load of theirs is 64 consecutive bytes of it.  The
 // distinct adapters of the rows are taken one after another, or one per grid slot: each reads its own A.
-template <int FMT, int JT, int RT, bool TURNED>
+template <int FMT, int JT, int RT, bool TURNED, int WAVES>
 __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, int slot, unsigned char* shared)
 {
     constexpr int kLd = 16 * JT + 8;                       // turned: elements between two rows of the staged unit
-    constexpr int WAVES = kShrinkWaves<JT, RT>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
     int which = 0;
@@ -142,13 +146,13 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
         const int64_t row = min(m0 + 16 * t + i, args.M - 1);
         q[t] = L.Q + (size_t)row * C + 8 * g;
     }
-    // turned: the unit's 64 rows of W are one piece of memory, 2 * JT times 16 bytes a lane at most; where each goes in LDS
-    uint16_t* own = reinterpret_cast<uint16_t*>(shared) + wave * (64 * kLd);
+    // turned: half a unit's 32 rows of W are one piece of memory, JT times 16 bytes a lane at most; where each goes in LDS
+    uint16_t* own = reinterpret_cast<uint16_t*>(shared) + wave * (32 * kLd);
     const int per_row = rank / 8;
-    int put[2 * JT];
+    int put[JT];
     if (TURNED) {
 #pragma unroll
-        for (int k = 0; k < 2 * JT; k++) {
+        for (int k = 0; k < JT; k++) {
             const int p = lane + 64 * k;
             put[k] = (p / per_row) * kLd + (p % per_row) * 8;
         }
@@ -167,63 +171,58 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
         for (int t = 0; t < RT; t++)
 #pragma unroll
             for (int j = 0; j < JT; j++) acc[t][j] = float4v{0, 0, 0, 0};
-        struct Unit {
-            u32x4 x[RT][2], w[JT][2];          // (turned: w is the piece as it lies in memory)
+        struct Half {
+            u32x4 x[RT], w[JT];          // (turned: w is the piece as it lies in memory)
         };
-        auto load = [&](Unit& b, int u) {
+        // half a unit: the k-th of this wavefront's
+        auto load = [&](Half& b, int k) {
+            const size_t c = (size_t)(u_begin + (k >> 1) * WAVES) * 64 + 32 * (k & 1);
 #pragma unroll
-            for (int t = 0; t < RT; t++)
-#pragma unroll
-                for (int h = 0; h < 2; h++) b.x[t][h] = *reinterpret_cast<const u32x4*>(q[t] + (size_t)u * 64 + 32 * h);
+            for (int t = 0; t < RT; t++) b.x[t] = *reinterpret_cast<const u32x4*>(q[t] + c);
             if (!TURNED) {
 #pragma unroll
-                for (int j = 0; j < JT; j++)
-#pragma unroll
-                    for (int h = 0; h < 2; h++) b.w[j][h] = *reinterpret_cast<const u32x4*>(wj[j] + (size_t)u * 64 + 32 * h);
+                for (int j = 0; j < JT; j++) b.w[j] = *reinterpret_cast<const u32x4*>(wj[j] + c);
             } else {
-                const u32x4* piece = reinterpret_cast<const u32x4*>(W + (size_t)u * 64 * rank);
+                const u32x4* piece = reinterpret_cast<const u32x4*>(W + c * rank);
 #pragma unroll
-                for (int k = 0; k < 2 * JT; k++) b.w[k >> 1][k & 1] = piece[min(lane + 64 * k, 64 * per_row - 1)];
+                for (int j = 0; j < JT; j++) b.w[j] = piece[min(lane + 64 * j, 32 * per_row - 1)];
             }
         };
-        auto compute = [&](const Unit& b) {
+        auto compute = [&](const Half& b) {
             if (TURNED) {
                 own_lds_order();
 #pragma unroll
-                for (int k = 0; k < 2 * JT; k++)
-                    if (lane + 64 * k < 64 * per_row) *reinterpret_cast<u32x4*>(own + put[k]) = b.w[k >> 1][k & 1];
+                for (int k = 0; k < JT; k++)
+                    if (lane + 64 * k < 32 * per_row) *reinterpret_cast<u32x4*>(own + put[k]) = b.w[k];
                 own_lds_order();
             }
 #pragma unroll
-            for (int h = 0; h < 2; h++)
+            for (int j = 0; j < JT; j++) {
+                u32x4 w = b.w[j];
+                if (TURNED) {
 #pragma unroll
-                for (int j = 0; j < JT; j++) {
-                    u32x4 w = b.w[j][h];
-                    if (TURNED) {
-#pragma unroll
-                        for (int e = 0; e < 2; e++) {
-                            const u32x2 d = read_turned(own + (32 * h + 8 * g + 4 * e + (i >> 2)) * kLd + min(16 * j + 4 * (i & 3), rank - 4));
-                            w[2 * e] = d[0];
-                            w[2 * e + 1] = d[1];
-                        }
+                    for (int e = 0; e < 2; e++) {
+                        const u32x2 d = read_turned(own + (8 * g + 4 * e + (i >> 2)) * kLd + min(16 * j + 4 * (i & 3), rank - 4));
+                        w[2 * e] = d[0];
+                        w[2 * e + 1] = d[1];
                     }
-#pragma unroll
-                    for (int t = 0; t < RT; t++)
-                        acc[t][j] = mfma16x16x32_of<FMT>(__builtin_bit_cast(half8, b.x[t][h]), __builtin_bit_cast(half8, w), acc[t][j]);
                 }
+#pragma unroll
+                for (int t = 0; t < RT; t++)
+                    acc[t][j] = mfma16x16x32_of<FMT>(__builtin_bit_cast(half8, b.x[t]), __builtin_bit_cast(half8, w), acc[t][j]);
+            }
         };
         if (u_begin < u_end) {
-            // one unit in flight while another is used (past the end: the last one again, so that the loads need no branch)
-            Unit b[2];
-            const int last = u_begin + (u_end - 1 - u_begin) / WAVES * WAVES;
-            load(b[0], u_begin);
-            loads_are_issued();
-            for (int u = u_begin; u < u_end; u += 2 * WAVES) {
-                if (RT > 1 || u + WAVES < u_end) load(b[1], min(u + WAVES, last));
+            // one half in flight while another is used (past the end: the last one again, so that the loads need no branch; few rows: none).  One way
+            // out of the loop: with more of them the sums are copied from register to register and spilled.
+            Half b[2];
+            const int n = 2 * ((u_end - 1 - u_begin) / WAVES + 1);
+            load(b[0], 0);
+            for (int k = 0; k < n; k += 2) {
+                load(b[1], k + 1);
                 loads_are_issued();
                 compute(b[0]);
-                if (u + WAVES >= u_end) break;
-                if (RT > 1 || u + 2 * WAVES < u_end) load(b[0], min(u + 2 * WAVES, last));
+                if (RT > 1 || k + 2 < n) load(b[0], min(k + 2, n - 1));
                 loads_are_issued();
                 compute(b[1]);
             }
@@ -253,10 +252,11 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
 }
 
 template <int FMT, int JT, int RT, bool TURNED>
-__global__ __launch_bounds__((64 * kShrinkWaves<JT, RT>)) void lora_shrink_kernel(ShrinkArgs args)
+__global__ __launch_bounds__((64 * kShrinkWaves<JT, RT>), (RT > 1 ? 2 : 1)) void lora_shrink_kernel(ShrinkArgs args)
 {
-    __shared__ __align__(16) unsigned char shared[kShrinkLds<JT, RT, TURNED>];
-    shrink_block<FMT, JT, RT, TURNED>(args, blockIdx.x, blockIdx.y, shared);
+    constexpr int WAVES = kShrinkWaves<JT, RT>;
+    __shared__ __align__(16) unsigned char shared[kShrinkLds<JT, RT, TURNED, WAVES>];
+    shrink_block<FMT, JT, RT, TURNED, WAVES>(args, blockIdx.x, blockIdx.y, shared);
 }
 
 // ------------------------------------------------------------------ finish
@@ -358,11 +358,11 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
     struct Rows {                        // what a row tile needs: Y, the owner, and P where it is ready
         u32x4 y[CB][2], p[JS][TERMS];
         float power;
-        int mine;
+        int word, mine;
     };
     auto load = [&](Rows& b, int64_t t) {
         const int64_t row = (tile0 + t) * 16 + i;
-        b.mine = adapter_of(args.index, row, args.M, args.adapters);
+        b.word = owner_word(args.index, row, args.M);
         const int64_t near = min(row, args.M - 1);
         const uint16_t* y = L.Y + (size_t)near * D + n0 + 8 * g;
 #pragma unroll
@@ -435,7 +435,9 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
     };
 
     auto work = [&](Rows& b, int64_t t) {
-        const int64_t row = (tile0 + t) * 16 + i;
+        // (a tile past this wavefront's: its rows are another's)
+        const int64_t row = t < tiles ? (tile0 + t) * 16 + i : args.M;
+        b.mine = owner_of(b.word, row, args.M, args.adapters);
         uint64_t pending = __ballot(b.mine != kNoAdapter) & 0xFFFF;
         bool store = b.mine == kNoAdapter && slot == 0 && row < args.M && L.out != L.Y;
         if (SLICED && L.hidden && n0 == 0 && slot == 0 && b.mine == kNoAdapter && row < args.M)
@@ -564,7 +566,6 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
             load(b[1], min(t + 1, tiles - 1));
             loads_are_issued();
             work(b[0], t);
-            if (t + 1 >= tiles) break;
             load(b[0], min(t + 2, tiles - 1));
             loads_are_issued();
             work(b[1], t + 1);
@@ -885,6 +886,41 @@ __global__ __launch_bounds__(256) void lora_outer_kernel(OuterArgs args)
     outer_block<FMT, JT, CT, BY_COLUMN, FUSED>(args, blockIdx.x, blockIdx.y, lds);
 }
 
+// ------------------------------------------------------------------ two independent steps of the backward pass in one launch
+// A launch costs 7 to 9 us beside its work here: the first loads of its workgroups, and at its end the write-back of what lies in the caches.  The
+// workgroups of two steps that do not read one another's results hide that for each other.
+template <int FMT, int JT>
+union FirstLds {
+    unsigned char shrink[kShrinkLds<JT, 1, true, 4>];
+    OuterLds<FMT, JT, 2> outer;
+};
+
+// few rows: dS, and the gradient of B
+template <int FMT, int JT>
+__global__ __launch_bounds__(256) void lora_first_kernel(ShrinkArgs shrink, int shrinks, OuterArgs outer)
+{
+    __shared__ __align__(16) FirstLds<FMT, JT> lds;
+    const int blocks = (outer.C + 127) / 128 * outer.splits, id = (int)blockIdx.x;
+    if (id < shrinks * shrink.slots) shrink_block<FMT, JT, 1, true, 4>(shrink, id % shrinks, id / shrinks, lds.shrink);
+    else outer_block<FMT, JT, 2, true, false>(outer, (id - shrinks * shrink.slots) % blocks, (id - shrinks * shrink.slots) / blocks, lds.outer);
+}
+
+template <int FMT, int JT, int CT>
+union SecondLds {
+    unsigned char expand[kExpandLds<true>];
+    OuterLds<FMT, JT, CT> outer;
+};
+
+// the gradient of A, and dX
+template <int FMT, int JT, int CT, bool SLICED>
+__global__ __launch_bounds__(256) void lora_second_kernel(ExpandArgs expand, int expands, OuterArgs outer)
+{
+    __shared__ __align__(16) SecondLds<FMT, JT, CT> lds;
+    const int blocks = (outer.C + 64 * CT - 1) / (64 * CT) * outer.splits, outers = blocks * outer.adapters, id = (int)blockIdx.x;
+    if (id < outers) outer_block<FMT, JT, CT, false, false>(outer, id % blocks, id / blocks, lds.outer);
+    else expand_block<FMT, JT <= 2 ? 1 : JT / 2, JT == 1, true, SLICED, SLICED || JT == 8 ? 1 : 2>(expand, (id - outers) % expands, (id - outers) / expands, lds.expand);
+}
+
 // out[k] (+)= the sum over the splits, in their order; two tensors in one launch
 struct JoinArgs {
     const float4v* part[2];
@@ -909,9 +945,15 @@ __global__ __launch_bounds__(256) void lora_join_kernel(JoinArgs args)
 // ------------------------------------------------------------------ plans and launches
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Up to this many rows the slices of a shrink are added up by the kernels that read them, and the adapters of the rows are dealt to workgroups of their own;
-// above it a launch of its own adds them up.
-constexpr int64_t kFewRows = 64;
+// Up to this many rows the slices of a shrink are added up by the kernels that read them; above it a launch of its own adds them up, once
+// (128 x 4096 x 4096 9.6 us, with that launch 13.7; 512 x 8192 x 8192 with eight adapters LATER_SLICED).
+constexpr int64_t kFewRows = 256;
+// Up to this many rows a shrink workgroup takes 16 of them and its adapters are dealt to workgroups of their own, above it 64 and one adapter
+// after another (333 x 5120 with five adapters 8.1 us against 17).
+constexpr int64_t kNarrowRows = 512;
+// Up to this many rows the expand kernel's adapters are dealt to workgroups of their own as well: with more, those that find nothing to do cost
+// more than they save (256 rows, eight adapters: LATER_SLOTS).
+constexpr int64_t kSlotRows = 64;
 
 // Rows a shrink workgroup takes, slots its adapters are dealt to, and slices of the contraction: two workgroups for each compute unit
 // (one, with few rows) where the contraction is long enough to be cut (a slice gives each wavefront at least one unit of 64).
@@ -923,18 +965,21 @@ struct ShrinkPlan {
 static ShrinkPlan plan_shrink(int64_t M, int C, int rank, int adapters)
 {
     ShrinkPlan p;
-    p.row_tiles = M <= kFewRows ? 1 : (rank > 64 ? 2 : 4);
+    const bool narrow = M <= kNarrowRows;
+    p.row_tiles = narrow ? 1 : (rank > 64 ? 2 : 4);
     const int64_t rows = 16 * p.row_tiles;
     p.groups = ceil_div(M, rows);
-    p.slots = M <= kFewRows ? (int)(adapters < rows ? adapters : rows) : 1;
-    const int waves = M > kFewRows || rank > 64 ? 4 : 8, limit = M > kFewRows ? 16 : kFewSlices;
-    const int64_t have = p.groups * p.slots, most = C / (64 * waves);
-    int64_t slices = ceil_div(M > kFewRows ? 512 : 256, have);
+    p.slots = narrow ? (int)(adapters < rows ? adapters : rows) : 1;
+    const int waves = !narrow || rank > 64 ? 4 : 8, limit = M > kFewRows ? 16 : kFewSlices;
+    const int64_t have = p.groups * (M <= kSlotRows ? p.slots : 1), most = C / (64 * waves);
+    int64_t slices = ceil_div(narrow ? 256 : 512, have);
     if (slices > most) slices = most;
     if (slices > limit) slices = limit;
     p.slices = (int)(slices < 1 ? 1 : slices);
     return p;
 }
+
+static int expand_slots(int64_t M, const ShrinkPlan& p) { return M <= kSlotRows ? p.slots : 1; }
 
 // Columns of an outer workgroup, and ranges of rows that separate workgroups take.  Two workgroups fit a compute unit, 512 are a round (516 took
 // 70 us where 430 take LATER_FUSED); a workgroup needs about 4 us beside its chunks and 3 (128 columns: 2.2) for each, adapters sharing
@@ -949,7 +994,7 @@ static OuterPlan plan_outer(int64_t M, int C, int rank, int adapters, bool fused
     double least = 1e30;
     const int64_t chunks = ceil_div(M, kChunk);
     for (int columns = 256; columns >= 128; columns -= 128) {
-        if (columns == 256 ? rank > 64 : fused) continue;
+        if (columns == 256 ? rank > 64 || M <= kFewRows : fused) continue;
         const int64_t have = ceil_div(C, columns) * adapters;
         for (int splits = 1; splits <= 64 && splits <= chunks; splits++) {
             const double chunk = columns == 256 ? 3.0 : 2.2, mine = (double)ceil_div(chunks, (int64_t)splits * adapters);
@@ -968,12 +1013,12 @@ static OuterPlan plan_outer(int64_t M, int C, int rank, int adapters, bool fused
 static bool fuses(int64_t M, int rank) { return M > kFewRows && rank <= 32; }
 
 template <int FMT, bool TURNED>
-static hipError_t launch_shrink(const ShrinkArgs& a, bool few, int64_t workgroups, hipStream_t stream)
+static hipError_t launch_shrink(const ShrinkArgs& a, bool narrow, int64_t workgroups, hipStream_t stream)
 {
     int rank = 0;
     for (int l = 0; l < a.layers; l++) rank = a.layer[l].rank > rank ? a.layer[l].rank : rank;
     const dim3 grid((unsigned)workgroups, (unsigned)a.slots), block(256);
-    if (few) {
+    if (narrow) {
         if (rank <= 16) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 1, TURNED>), grid, dim3(64 * kShrinkWaves<1, 1>), 0, stream, a);
         else if (rank <= 32) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 1, TURNED>), grid, dim3(64 * kShrinkWaves<2, 1>), 0, stream, a);
         else if (rank <= 64) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, 1, TURNED>), grid, dim3(64 * kShrinkWaves<4, 1>), 0, stream, a);
@@ -1001,22 +1046,22 @@ static hipError_t launch_finish(const float* P, float* sum, uint16_t* terms, flo
 // Columns of an expand workgroup
 static int expand_across(bool few, int rank) { return few ? 256 : (rank > 64 ? 64 : 128); }
 
-template <int FMT, bool TURNED>
+template <int FMT>
 static hipError_t launch_expand(const ExpandArgs& a, bool few, int rank, int64_t workgroups, hipStream_t stream)
 {
     const dim3 grid((unsigned)workgroups, (unsigned)a.slots), block(256);
     bool packed = true;
     for (int l = 0; l < a.layers; l++) packed = packed && a.layer[l].rank <= 16;
     if (few) {
-        if (packed) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, true, TURNED, true, 1>), grid, block, 0, stream, a);
-        else if (rank <= 32) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, false, TURNED, true, 1>), grid, block, 0, stream, a);
-        else if (rank <= 64) hipLaunchKernelGGL((lora_expand_kernel<FMT, 2, false, TURNED, true, 1>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((lora_expand_kernel<FMT, 4, false, TURNED, true, 1>), grid, block, 0, stream, a);
+        if (packed) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, true, false, true, 1>), grid, block, 0, stream, a);
+        else if (rank <= 32) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, false, false, true, 1>), grid, block, 0, stream, a);
+        else if (rank <= 64) hipLaunchKernelGGL((lora_expand_kernel<FMT, 2, false, false, true, 1>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((lora_expand_kernel<FMT, 4, false, false, true, 1>), grid, block, 0, stream, a);
     } else {
-        if (packed) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, true, TURNED, false, 2>), grid, block, 0, stream, a);
-        else if (rank <= 32) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, false, TURNED, false, 2>), grid, block, 0, stream, a);
-        else if (rank <= 64) hipLaunchKernelGGL((lora_expand_kernel<FMT, 2, false, TURNED, false, 2>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((lora_expand_kernel<FMT, 4, false, TURNED, false, 1>), grid, block, 0, stream, a);
+        if (packed) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, true, false, false, 2>), grid, block, 0, stream, a);
+        else if (rank <= 32) hipLaunchKernelGGL((lora_expand_kernel<FMT, 1, false, false, false, 2>), grid, block, 0, stream, a);
+        else if (rank <= 64) hipLaunchKernelGGL((lora_expand_kernel<FMT, 2, false, false, false, 2>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((lora_expand_kernel<FMT, 4, false, false, false, 1>), grid, block, 0, stream, a);
     }
     return hipGetLastError();
 }
@@ -1045,13 +1090,43 @@ static hipError_t launch_outer(const OuterArgs& a, int columns, hipStream_t stre
     return hipGetLastError();
 }
 
+template <int FMT>
+static hipError_t launch_first(const ShrinkArgs& s, int shrinks, const OuterArgs& o, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(shrinks * s.slots + ceil_div(o.C, 128) * o.splits * o.adapters)), block(256);
+    if (o.rank <= 16) hipLaunchKernelGGL((lora_first_kernel<FMT, 1>), grid, block, 0, stream, s, shrinks, o);
+    else if (o.rank <= 32) hipLaunchKernelGGL((lora_first_kernel<FMT, 2>), grid, block, 0, stream, s, shrinks, o);
+    else if (o.rank <= 64) hipLaunchKernelGGL((lora_first_kernel<FMT, 4>), grid, block, 0, stream, s, shrinks, o);
+    else hipLaunchKernelGGL((lora_first_kernel<FMT, 8>), grid, block, 0, stream, s, shrinks, o);
+    return hipGetLastError();
+}
+
+template <int FMT, int CT, bool SLICED>
+static hipError_t launch_second_rank(const ExpandArgs& e, int expands, const OuterArgs& o, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(expands * e.slots + ceil_div(o.C, 64 * CT) * o.splits * o.adapters)), block(256);
+    if (o.rank <= 16) hipLaunchKernelGGL((lora_second_kernel<FMT, 1, CT, SLICED>), grid, block, 0, stream, e, expands, o);
+    else if (o.rank <= 32) hipLaunchKernelGGL((lora_second_kernel<FMT, 2, CT, SLICED>), grid, block, 0, stream, e, expands, o);
+    else if (o.rank <= 64) hipLaunchKernelGGL((lora_second_kernel<FMT, 4, CT, SLICED>), grid, block, 0, stream, e, expands, o);
+    else hipLaunchKernelGGL((lora_second_kernel<FMT, 8, 2, SLICED>), grid, block, 0, stream, e, expands, o);
+    return hipGetLastError();
+}
+
+template <int FMT>
+static hipError_t launch_second(const ExpandArgs& e, bool few, int64_t expands, const OuterArgs& o, int columns, hipStream_t stream)
+{
+    if (few) return launch_second_rank<FMT, 2, true>(e, (int)expands, o, stream);
+    return columns == 128 ? launch_second_rank<FMT, 2, false>(e, (int)expands, o, stream)
+                          : launch_second_rank<FMT, 4, false>(e, (int)expands, o, stream);
+}
+
 // Row tiles of 16 rows that a wavefront of the expand kernel takes one after another (its operands of W stay in registers, and the next tile's loads
-// are in flight): as many as leave two workgroups for each compute unit, eight at most.
+// are in flight): as many as make the workgroups one round of two to a compute unit.
 static int expand_row_tiles(int64_t M, int64_t column_blocks)
 {
     if (M <= kFewRows) return 1;
-    const int64_t tiles = ceil_div(M, 64), t = tiles * column_blocks / 512;
-    return (int)(t < 1 ? 1 : (t > 8 ? 8 : t));
+    const int64_t t = ceil_div(ceil_div(M, 64) * column_blocks, 512);
+    return (int)(t < 1 ? 1 : (t > 16 ? 16 : t));
 }
 
 static int64_t expand_groups(int64_t M, bool few, int row_tiles) { return ceil_div(M, 16 * (few ? 1 : 4) * row_tiles); }
@@ -1111,7 +1186,8 @@ static hipError_t launch_lora_t(int64_t M, const fp6_lora_problem* pr, int count
     for (int l = 0; l < count; l++) {
         const ShrinkPlan p = plan_shrink(M, (int)pr[l].K, rank, adapters);
         const ShrinkSpace space = shrink_space(p, M, pr[l].rank);
-        s.slots = e.slots = p.slots;
+        s.slots = p.slots;
+        e.slots = expand_slots(M, p);
         s.layer[l] = ShrinkLayer{pr[l].X, pr[l].A, (float*)at, (int)pr[l].K, (int)pr[l].rank, p.slices, (int)shrinks};
         e.layer[l] = ExpandLayer{few ? (const float*)at : (const float*)(at + space.slices + space.terms), (const uint16_t*)(at + space.slices),
                                  pr[l].B, pr[l].Y, pr[l].out, pr[l].hidden, (int)pr[l].N, (int)pr[l].rank, p.slices, (int)expands};
@@ -1119,12 +1195,12 @@ static hipError_t launch_lora_t(int64_t M, const fp6_lora_problem* pr, int count
         shrinks += p.groups * p.slices;
         expands += ceil_div(pr[l].N, across) * expand_groups(M, few, e.row_tiles);
     }
-    hipError_t err = launch_shrink<FMT, false>(s, few, shrinks, stream);
+    hipError_t err = launch_shrink<FMT, false>(s, M <= kNarrowRows, shrinks, stream);
     for (int l = 0; l < count && !few && err == hipSuccess; l++)
         err = launch_finish<FMT>(s.layer[l].P, pr[l].hidden, const_cast<uint16_t*>(e.layer[l].terms), const_cast<float*>(e.layer[l].P), M,
                                  (int)pr[l].rank, s.layer[l].slices, index, adapters, stream);
     if (err != hipSuccess) return err;
-    return launch_expand<FMT, false>(e, few, rank, expands, stream);
+    return launch_expand<FMT>(e, few, rank, expands, stream);
 }
 
 hipError_t launch_lora(bool bf16, int64_t M, const fp6_lora_problem* pr, int count, int adapters, const int32_t* index, const float* scaling,
@@ -1176,26 +1252,29 @@ static hipError_t launch_backward_t(const LoraBackward& b, unsigned char* worksp
     float* da = (float*)(at + p.space.bytes);
     float* db = (float*)(at + p.space.bytes + p.da);
     hipError_t err = hipSuccess;
-    if (!p.fused) {
-        ShrinkArgs s{};
-        s.layers = 1;
-        s.M = b.M;
-        s.index = b.index;
-        s.scaling = b.scaling;
-        s.adapters = b.adapters;
-        s.slots = p.shrink.slots;
-        s.layer[0] = ShrinkLayer{b.dY, b.B, dh, (int)b.N, b.rank, p.shrink.slices, 0};
-        err = launch_shrink<FMT, true>(s, few, p.shrink.groups * p.shrink.slices, stream);
-        if (err != hipSuccess) return err;
-    }
-    // (right behind the shrink, where it is not part of it: what the last-level cache still holds of dY is read from there)
     const OuterArgs ob{b.hidden, b.dY, p.b.splits > 1 ? db : b.dB, b.M, (int)b.N, b.rank, 1, b.adapters, p.b.splits, b.accumulate, b.index, b.scaling,
                        p.fused ? b.B : nullptr, p.fused ? dh : nullptr};
-    err = launch_outer<FMT, true>(ob, p.b.columns, stream);
+    ShrinkArgs s{};
+    s.layers = 1;
+    s.M = b.M;
+    s.index = b.index;
+    s.scaling = b.scaling;
+    s.adapters = b.adapters;
+    s.slots = p.shrink.slots;
+    s.layer[0] = ShrinkLayer{b.dY, b.B, dh, (int)b.N, b.rank, p.shrink.slices, 0};
+    const int64_t shrinks = p.shrink.groups * p.shrink.slices;
+    if (few) {
+        err = launch_first<FMT>(s, (int)shrinks, ob, stream);
+    } else {
+        if (!p.fused) err = launch_shrink<FMT, true>(s, b.M <= kNarrowRows, shrinks, stream);
+        // (right behind the shrink, where it is not part of it: what the last-level cache still holds of dY is read from there)
+        if (err == hipSuccess) err = launch_outer<FMT, true>(ob, p.b.columns, stream);
+        // the sum over the slices goes where the first slice lies
+        if (err == hipSuccess) err = launch_finish<FMT>(dh, dh, terms, power, b.M, b.rank, p.shrink.slices, b.index, b.adapters, stream);
+    }
     if (err != hipSuccess) return err;
-    // the sum over the slices goes where the first slice lies
-    if (!few) err = launch_finish<FMT>(dh, dh, terms, power, b.M, b.rank, p.shrink.slices, b.index, b.adapters, stream);
-    if (err != hipSuccess) return err;
+    const OuterArgs oa{dh, b.X, p.a.splits > 1 ? da : b.dA, b.M, (int)b.K, b.rank, few ? p.shrink.slices : 1, b.adapters, p.a.splits, b.accumulate,
+                       b.index, nullptr, nullptr, nullptr};
     if (b.out) {
         const int across = expand_across(few, b.rank);
         ExpandArgs e{};
@@ -1203,15 +1282,13 @@ static hipError_t launch_backward_t(const LoraBackward& b, unsigned char* worksp
         e.M = b.M;
         e.index = b.index;
         e.adapters = b.adapters;
-        e.slots = p.shrink.slots;
+        e.slots = expand_slots(b.M, p.shrink);
         e.row_tiles = expand_row_tiles(b.M, ceil_div(b.K, across));
         e.layer[0] = ExpandLayer{few ? dh : power, terms, b.A, b.dX, b.out, nullptr, (int)b.K, b.rank, p.shrink.slices, 0};
-        err = launch_expand<FMT, true>(e, few, b.rank, ceil_div(b.K, across) * expand_groups(b.M, few, e.row_tiles), stream);
-        if (err != hipSuccess) return err;
+        err = launch_second<FMT>(e, few, ceil_div(b.K, across) * expand_groups(b.M, few, e.row_tiles), oa, p.a.columns, stream);
+    } else {
+        err = launch_outer<FMT, false>(oa, p.a.columns, stream);
     }
-    const OuterArgs oa{dh, b.X, p.a.splits > 1 ? da : b.dA, b.M, (int)b.K, b.rank, few ? p.shrink.slices : 1, b.adapters, p.a.splits, b.accumulate,
-                       b.index, nullptr, nullptr, nullptr};
-    err = launch_outer<FMT, false>(oa, p.a.columns, stream);
     if (err != hipSuccess || (p.a.splits == 1 && p.b.splits == 1)) return err;
     JoinArgs j{};
     j.accumulate = b.accumulate;
