@@ -140,12 +140,6 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
         for (int e = threadIdx.x; e < 16 * RT * rank; e += 64 * WAVES)
             if ((none >> (e / rank)) & 1 && m0 + e / rank < args.M) P[(size_t)(m0 + e / rank) * rank + e % rank] = 0.0f;
     }
-    const uint16_t* q[RT];
-#pragma unroll
-    for (int t = 0; t < RT; t++) {
-        const int64_t row = min(m0 + 16 * t + i, args.M - 1);
-        q[t] = L.Q + (size_t)row * C + 8 * g;
-    }
     // turned: half a unit's 32 rows of W are one piece of memory, JT times 16 bytes a lane at most; where each goes in LDS
     uint16_t* own = reinterpret_cast<uint16_t*>(shared) + wave * (32 * kLd);
     const int per_row = rank / 8;
@@ -162,6 +156,14 @@ __device__ __forceinline__ void shrink_block(const ShrinkArgs& args, int block, 
         const uint64_t rows = __ballot(mine == a);
         pending &= ~rows;
         if (seen % args.slots != slot) continue;
+        // (lanes of other rows read one that is this adapter's: what they add up is dropped)
+        const int some = __builtin_ctzll(rows);
+        const uint16_t* q[RT];
+#pragma unroll
+        for (int t = 0; t < RT; t++) {
+            const int row = (rows >> (16 * t + i)) & 1 ? 16 * t + i : some;
+            q[t] = L.Q + (size_t)(m0 + row) * C + 8 * g;
+        }
         const uint16_t* W = L.W + (size_t)a * rank * C;
         const uint16_t* wj[JT];
 #pragma unroll
@@ -360,11 +362,8 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
         float power;
         int word, mine;
     };
-    auto load = [&](Rows& b, int64_t t) {
-        const int64_t row = (tile0 + t) * 16 + i;
-        b.word = owner_word(args.index, row, args.M);
-        const int64_t near = min(row, args.M - 1);
-        const uint16_t* y = L.Y + (size_t)near * D + n0 + 8 * g;
+    auto load_y = [&](Rows& b, int64_t row) {
+        const uint16_t* y = L.Y + (size_t)row * D + n0 + 8 * g;
 #pragma unroll
         for (int c = 0; c < CB; c++)
 #pragma unroll
@@ -372,7 +371,22 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
                 const int off = 64 * c + 32 * h;
                 b.y[c][h] = *reinterpret_cast<const u32x4*>(y + (n0 + off < D ? off : 0));
             }
+    };
+    auto store_y = [&](const Rows& b, int64_t row) {
+        uint16_t* to = L.out + (size_t)row * D + n0 + 8 * g;
+#pragma unroll
+        for (int c = 0; c < CB; c++)
+            if (n0 + 64 * c < D) {
+                *reinterpret_cast<u32x4*>(to + 64 * c) = b.y[c][0];
+                *reinterpret_cast<u32x4*>(to + 64 * c + 32) = b.y[c][1];
+            }
+    };
+    auto load = [&](Rows& b, int64_t t) {
+        const int64_t row = (tile0 + t) * 16 + i;
+        b.word = owner_word(args.index, row, args.M);
+        const int64_t near = min(row, args.M - 1);
         if (!SLICED) {
+            load_y(b, near);
             const uint16_t* p = L.terms + (size_t)near * 2 * rank;
             b.power = FMT != kE3M2B ? L.P[near] : 1.0f;
 #pragma unroll
@@ -439,14 +453,25 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
         const int64_t row = t < tiles ? (tile0 + t) * 16 + i : args.M;
         b.mine = owner_of(b.word, row, args.M, args.adapters);
         uint64_t pending = __ballot(b.mine != kNoAdapter) & 0xFFFF;
-        bool store = b.mine == kNoAdapter && slot == 0 && row < args.M && L.out != L.Y;
+        bool store = !SLICED && b.mine == kNoAdapter && slot == 0 && row < args.M && L.out != L.Y;
+        if (SLICED && b.mine == kNoAdapter && slot == 0 && row < args.M && L.out != L.Y) {
+            // (few rows: Y is read for the adapter at hand, these are copied by themselves)
+            const u32x4* from = reinterpret_cast<const u32x4*>(L.Y + (size_t)row * D + n0 + 8 * g);
+            u32x4* to = reinterpret_cast<u32x4*>(L.out + (size_t)row * D + n0 + 8 * g);
+            const u32x4 y0 = from[0], y1 = from[4];
+            to[0] = y0;
+            to[4] = y1;
+        }
         if (SLICED && L.hidden && n0 == 0 && slot == 0 && b.mine == kNoAdapter && row < args.M)
             for (int j = 4 * g; j < rank; j += 16) *reinterpret_cast<float4v*>(L.hidden + (size_t)row * rank + j) = float4v{0, 0, 0, 0};
         for (int seen = 0; pending; seen++) {
-            const int a = __builtin_amdgcn_readlane(b.mine, __builtin_ctzll(pending));
+            const int some = __builtin_ctzll(pending), a = __builtin_amdgcn_readlane(b.mine, some);
             pending &= ~(__ballot(b.mine == a) & 0xFFFF);
             if (seen % args.slots != slot) continue;
             if (SLICED) {
+                // (lanes of other rows read one that is this adapter's: nothing of theirs is stored)
+                const int64_t from = b.mine == a ? row : tile0 * 16 + some;
+                load_y(b, from);
                 // P of this lane's row, eight values per step: the slices are asked for together, and W behind them
                 float v[JS][8];
                 float top = 0.0f;
@@ -454,7 +479,7 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
                 for (int s = 0; s < JS; s++) {
                     const int k0 = 32 * s + 8 * g, j0 = PACKED && k0 >= rank ? k0 - rank : k0;
                     const bool real = b.mine == a && j0 < rank;
-                    const float* p = L.P + (size_t)min(row, args.M - 1) * rank + min(j0, rank - 8);
+                    const float* p = L.P + (size_t)from * rank + min(j0, rank - 8);
                     const size_t step = (size_t)args.M * rank;
                     float4v lo[kFewSlices], hi[kFewSlices];
 #pragma unroll
@@ -538,16 +563,9 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
                     store = true;
                 }
             }
+            if (SLICED && b.mine == a) store_y(b, row);
         }
-        if (store) {
-            uint16_t* to = L.out + (size_t)row * D + n0 + 8 * g;
-#pragma unroll
-            for (int c = 0; c < CB; c++)
-                if (n0 + 64 * c < D) {
-                    *reinterpret_cast<u32x4*>(to + 64 * c) = b.y[c][0];
-                    *reinterpret_cast<u32x4*>(to + 64 * c + 32) = b.y[c][1];
-                }
-        }
+        if (!SLICED && store) store_y(b, row);
     };
 
     if (SLICED) {
