@@ -14,8 +14,6 @@
 
 namespace fp6 {
 
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-
 // 32 bits from x = number of the element * 0x9E3779B1 + t * 0x3C6EF373 + seed: two rounds of xor-shift and multiplication (by the fractional
 // parts of the golden ratio and of the roots of 5, 2 and 3).
 __device__ __forceinline__ uint32_t counter_hash(uint32_t x)

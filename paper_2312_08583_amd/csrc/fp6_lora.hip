@@ -12,8 +12,6 @@
 
 namespace fp6 {
 
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kNoAdapter = -1;
 
 // The adapter of a row, or kNoAdapter: what index holds for it (of the last row past the end: the load takes no branch), and whether that is one.
@@ -264,7 +262,7 @@ __global__ __launch_bounds__((64 * kShrinkWaves<JT, RT>), (RT > 1 ? 2 : 1)) void
 // ------------------------------------------------------------------ finish
 struct FinishArgs {
     const float* P;          // [slices, M, rank]
-    float* sum;              // [M, rank]: the slices added up (NULL: not wanted; may be P)
+    float* sum;              // [M, rank]: the slices added up (NULL: not wanted; may be P: every row is read by the workgroup that writes it)
     uint16_t* terms;         // [M][2][rank]: the sum as two 16-bit terms of a row times 2^exponent
     float* power;            // [M]: 2^exponent
     int64_t M;
@@ -273,24 +271,32 @@ struct FinishArgs {
     int adapters;
 };
 
-// The slices of the contraction added up, in their order, and split into the two terms that the expand kernel multiplies with: once a row
-// instead of once a row and block of columns.
-template <int FMT>
+// The slices of the contraction added up, and split into the two terms that the expand kernel multiplies with: once a row instead of once a row
+// and block of columns.  MANY slices: the four wavefronts of a workgroup take every fourth slice of the same rows, and their sums are added in
+// their order (4096 rows, 86 slices of rank 16: 6.2 us, 8.5 with a thread for all slices; 512 rows, 8 slices: 4.6 and 3.3).
+template <int FMT, bool MANY>
 __global__ __launch_bounds__(256) void lora_finish_kernel(FinishArgs args)
 {
-    const int lanes = args.lanes, rank = args.rank;
-    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
-    const int j = 4 * (int)(threadIdx.x % lanes);
-    const bool real = row < args.M && j < rank, owned = real && adapter_of(args.index, row, args.M, args.adapters) != kNoAdapter;
+    __shared__ float4v meet[MANY ? 3 : 1][64];
+    const int lanes = args.lanes, rank = args.rank, lane = threadIdx.x & 63, wave = MANY ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    const int64_t row = ((int64_t)blockIdx.x * (MANY ? 64 : 256) + (MANY ? lane : (int)threadIdx.x)) / lanes;
+    const int j = 4 * (lane % lanes);
+    const bool real = row < args.M && j < rank;
+    const int word = owner_word(args.index, row, args.M);
     float4v v = float4v{0, 0, 0, 0};
-    if (real) {
-        const float* p = args.P + (size_t)row * rank + j;
-        const size_t step = (size_t)args.M * rank;
+    const float* p = args.P + (size_t)min(row, args.M - 1) * rank + min(j, rank - 4);
+    const size_t step = (size_t)args.M * rank;
 #pragma unroll 8
-        for (int c = 0; c < args.slices; c++) v += *reinterpret_cast<const float4v*>(p + c * step);
-        if (!owned) v = float4v{0, 0, 0, 0};
-        if (args.sum) *reinterpret_cast<float4v*>(args.sum + (size_t)row * rank + j) = v;
+    for (int c = wave; c < args.slices; c += MANY ? 4 : 1) v += *reinterpret_cast<const float4v*>(p + c * step);
+    if (MANY) {
+        if (wave) meet[wave - 1][lane] = v;
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int w = 0; w < 3; w++) v += meet[w][lane];
     }
+    if (!real || owner_of(word, row, args.M, args.adapters) == kNoAdapter) v = float4v{0, 0, 0, 0};
+    if (real && args.sum) *reinterpret_cast<float4v*>(args.sum + (size_t)row * rank + j) = v;
     int exponent = 0;
     if (FMT != kE3M2B) {
         float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
@@ -329,7 +335,7 @@ struct ExpandArgs {
     int64_t M;
     const int32_t* index;
     const float* scaling;
-    int adapters, slots, row_tiles;      // row tiles of 16 rows per workgroup
+    int adapters, slots, row_tiles;      // row tiles of 16 rows per wavefront
 };
 
 constexpr int kExpandLd = 64 + 8;        // turned: elements between two rows of a staged piece of W
@@ -934,6 +940,7 @@ template <int FMT, int JT, int CT, bool SLICED>
 __global__ __launch_bounds__(256) void lora_second_kernel(ExpandArgs expand, int expands, OuterArgs outer)
 {
     __shared__ __align__(16) SecondLds<FMT, JT, CT> lds;
+    // (in turn, a workgroup of the one beside one of the other, they take longer: 56 us become 59, at rank 128 120 become 157)
     const int blocks = (outer.C + 64 * CT - 1) / (64 * CT) * outer.splits, outers = blocks * outer.adapters, id = (int)blockIdx.x;
     if (id < outers) outer_block<FMT, JT, CT, false, false>(outer, id % blocks, id / blocks, lds.outer);
     else expand_block<FMT, JT <= 2 ? 1 : JT / 2, JT == 1, true, SLICED, SLICED || JT == 8 ? 1 : 2>(expand, (id - outers) % expands, (id - outers) / expands, lds.expand);
@@ -964,13 +971,14 @@ __global__ __launch_bounds__(256) void lora_join_kernel(JoinArgs args)
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Up to this many rows the slices of a shrink are added up by the kernels that read them; above it a launch of its own adds them up, once
-// (128 x 4096 x 4096 9.6 us, with that launch 13.7; 512 x 8192 x 8192 with eight adapters LATER_SLICED).
+// (128 x 4096 x 4096 9.6 us, with that launch 13.7; 333 x 13824 x 5120 with five adapters 27 and 23, gradients of 512 x 8192 x 8192, rank 64,
+// 55 and 45).
 constexpr int64_t kFewRows = 256;
 // Up to this many rows a shrink workgroup takes 16 of them and its adapters are dealt to workgroups of their own, above it 64 and one adapter
 // after another (333 x 5120 with five adapters 8.1 us against 17).
 constexpr int64_t kNarrowRows = 512;
 // Up to this many rows the expand kernel's adapters are dealt to workgroups of their own as well: with more, those that find nothing to do cost
-// more than they save (256 rows, eight adapters: LATER_SLOTS).
+// more than they save (256 x 8192 with eight adapters 15.9 us, here 10.4).
 constexpr int64_t kSlotRows = 64;
 
 // Rows a shrink workgroup takes, slots its adapters are dealt to, and slices of the contraction: two workgroups for each compute unit
@@ -1000,7 +1008,7 @@ static ShrinkPlan plan_shrink(int64_t M, int C, int rank, int adapters)
 static int expand_slots(int64_t M, const ShrinkPlan& p) { return M <= kSlotRows ? p.slots : 1; }
 
 // Columns of an outer workgroup, and ranges of rows that separate workgroups take.  Two workgroups fit a compute unit, 512 are a round (516 took
-// 70 us where 430 take LATER_FUSED); a workgroup needs about 4 us beside its chunks and 3 (128 columns: 2.2) for each, adapters sharing
+// 70 us where 430 take 54: the last four had a round to themselves); a workgroup needs about 4 us beside its chunks and 3 (128 columns: 2.2) for each, adapters sharing
 // the rows evenly; every range costs a tensor of partial sums, written and read at 4 TB/s, and together they cost a launch.
 struct OuterPlan {
     int columns, splits;
@@ -1057,7 +1065,8 @@ static hipError_t launch_finish(const float* P, float* sum, uint16_t* terms, flo
     int lanes = 2;
     while (4 * lanes < rank) lanes *= 2;
     const FinishArgs f{P, sum, terms, power, M, rank, slices, lanes, index, adapters};
-    hipLaunchKernelGGL(lora_finish_kernel<FMT>, dim3((unsigned)ceil_div(M * lanes, 256)), dim3(256), 0, stream, f);
+    if (slices > 32) hipLaunchKernelGGL((lora_finish_kernel<FMT, true>), dim3((unsigned)ceil_div(M * lanes, 64)), dim3(256), 0, stream, f);
+    else hipLaunchKernelGGL((lora_finish_kernel<FMT, false>), dim3((unsigned)ceil_div(M * lanes, 256)), dim3(256), 0, stream, f);
     return hipGetLastError();
 }
 
