@@ -414,12 +414,13 @@ int fp6_linear_v2_bf16(const uint16_t *X, int64_t M, const void *hi_plane, const
  *           of out is the row of Y, bit for bit, whatever X holds there.  Rows may come in any order; rows of one adapter
  *           that are neighbours are cheapest.
  *   scaling fp32 [adapters] on the device, or NULL: 1
- *   rank    8 .. FP6_LORA_RANK_MAX, a multiple of 8 (adapters of a lower rank: rows of zeros)
+ *   rank    8 .. FP6_LORA_RANK_MAX, a multiple of 8 (adapters of a lower rank: rows of zeros); adapters 1 .. 65535
  *   workspace  >= fp6_lora_workspace_bytes; the contract of fp6_linear's workspace: its first FP6_WORKSPACE_ZERO_BYTES bytes are
  *           left as they are (so one buffer serves both), the rest need not be zero.  Calls that share it must not overlap in time.
  * fp6_lora_group: up to FP6_GROUP_MAX projections of the same rows (q, k and v; gate and up) in the same two launches; the rows'
  * adapters and the scaling are common, N, K and rank may differ.  No out may overlap what another layer of the group reads.
- * An infinity or NaN in a row of X stays in that row.  Errors: FP6_ERR_NULL, FP6_ERR_SHAPE, FP6_ERR_ALIGN, FP6_ERR_VALUE (type,
+ * An infinity or NaN in a row of X stays in that row.  Errors: FP6_ERR_NULL, FP6_ERR_SHAPE (also M > 2^24, and sizes that need more
+ * workgroups than a launch can have), FP6_ERR_ALIGN, FP6_ERR_VALUE (type,
  * rank, adapters), FP6_ERR_OVERLAP, FP6_ERR_WORKSPACE, FP6_ERR_HIP.
  */
 typedef struct fp6_lora_problem {
@@ -487,9 +488,10 @@ int fp6_linear_grad(int format, const uint16_t *dY, int64_t M, const void *hi_t,
  * caller copies it to 16-byte aligned device memory once and keeps it as long as the tensors stay where they are.  It refuses
  * NULL (FP6_ERR_NULL), misaligned (16 bytes; scale bytes: any; FP6_ERR_ALIGN) and overlapping (FP6_ERR_OVERLAP: what is
  * written twice, or written and read as a gradient) tensors; a count of 0 is fine.  `items` receives what fp6_adamw wants to know.
- * One call at a time may use a plan.  lr may come from the device (lr_device != NULL: it counts instead of lr), as may grad_scale
- * (NULL: 1; the inverse of a loss scale, a clipping factor); found_inf (NULL: never): where it is not 0 the call changes nothing,
- * not even step.  So a captured call can be replayed as step, learning rate and scale move on.
+ * One call at a time may use a plan; a plan of other state_bits than the call says, or what is no plan: nothing is changed.
+ * lr may come from the device (lr_device != NULL: it counts instead of lr), as may grad_scale (NULL: 1; the inverse of a loss
+ * scale, a clipping factor); found_inf (NULL: never): where it is not 0 the call changes nothing, not even step.  So a captured
+ * call can be replayed as step, learning rate and scale move on.
  * FP6_ERR_VALUE: beta outside [0, 1), negative or non-finite lr, eps or weight_decay, state_bits, types, items.
  */
 typedef struct fp6_adamw_tensor {

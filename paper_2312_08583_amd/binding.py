@@ -850,22 +850,22 @@ def fp6_adamw_plan(params, grads, first, second, first_scales=None, second_scale
     if grads[0].dtype not in _TYPE or (copies is not None and copies[0].dtype not in (torch.float16, torch.bfloat16)):
         raise Fp6Error("grads must be fp32, fp16 or bf16, copies fp16 or bf16")
     call = _Call(params[0], "param")
-    arr = (AdamWTensor * n)()
-    for i in range(n):
-        p, count = params[i], params[i].numel()
+    counts = [t.numel() for t in params]
+    blocks = [-(-c // 256) for c in counts]
 
-        def like(t, dtype, what):
-            ptr = call.ptr(t, dtype, what)
-            if t.numel() != count:
-                raise Fp6Error("%s %d holds %d elements, its param %d" % (what, i, t.numel(), count))
-            return ptr
+    def pointers(tensors, dtype, what, sizes):
+        if tensors is None:
+            return [None] * n
+        for i, (t, size) in enumerate(zip(tensors, sizes)):
+            if not t.is_cuda or t.dtype != dtype or t.device != call.device or not t.is_contiguous() or t.numel() != size:
+                call.flat(t, dtype, "%s %d" % (what, i), size)          # says which of them it is
+        return [t.data_ptr() for t in tensors]
 
-        blocks = (-(-count // 256),)
-        arr[i] = AdamWTensor(call.ptr(p, torch.float32, "param"), like(grads[i], grads[0].dtype, "grad"), like(first[i], state, "first"),
-                             like(second[i], state, "second"),
-                             call.ptr(first_scales[i], torch.uint8, "first_scales", blocks) if eight else None,
-                             call.ptr(second_scales[i], torch.uint8, "second_scales", blocks) if eight else None,
-                             like(copies[i], copies[0].dtype, "copy") if copies is not None else None, count)
+    columns = [pointers(params, torch.float32, "param", counts), pointers(grads, grads[0].dtype, "grad", counts),
+               pointers(first, state, "first", counts), pointers(second, state, "second", counts),
+               pointers(first_scales, torch.uint8, "first_scales", blocks), pointers(second_scales, torch.uint8, "second_scales", blocks),
+               pointers(copies, copies[0].dtype if copies is not None else None, "copy", counts), counts]
+    arr = (AdamWTensor * n)(*map(AdamWTensor, *columns))
     bits, grad_type = 8 if eight else 32, _TYPE[grads[0].dtype]
     copy_type = FP6_NO_COPY if copies is None else _TYPE[copies[0].dtype]
     host = torch.zeros(int(lib().fp6_adamw_plan_bytes(arr, n)), dtype=torch.uint8)

@@ -42,11 +42,16 @@ static int lora_numbers(int type, int64_t rank, int64_t adapters)
     return FP6_OK;
 }
 
-// Workgroups of the launches are counted in 31 bits.
-static bool lora_fits(int64_t M, int64_t columns) { return (M + 15) / 16 * ((columns + 255) / 256) < (int64_t)1 << 28; }
+// The threads of a launch are counted in 32 bits, its workgroups of 256 in 24: half of them for each of the steps that share a launch.  (Up to
+// 512 rows workgroups take at least 16 rows and 256 columns, adapters may be dealt to 16 of them; above, with so many, 1024 rows and 64 columns.)
+static bool lora_fits(int64_t M, int64_t columns, int64_t adapters)
+{
+    const int64_t few = (M + 15) / 16 * ((columns + 255) / 256) * std::min<int64_t>(adapters, 16), many = (M + 1023) / 1024 * ((columns + 63) / 64);
+    return (M <= 512 ? few : many) < (int64_t)1 << 22;
+}
 static bool backward_fits(int64_t M, int64_t N, int64_t K, int64_t adapters)
 {
-    return lora_fits(M, std::max(N, K)) && (std::max(N, K) + 127) / 128 * adapters < (int64_t)1 << 24;
+    return lora_fits(M, std::max(N, K), adapters) && (std::max(N, K) + 127) / 128 * adapters < (int64_t)1 << 23;
 }
 
 static int lora_check(int type, int64_t M, const fp6_lora_problem* pr, int count, int64_t adapters)
@@ -60,7 +65,7 @@ static int lora_check(int type, int64_t M, const fp6_lora_problem* pr, int count
         if (!shape_ok(pr[i].N, pr[i].K)) return FP6_ERR_SHAPE;
         columns += pr[i].N;
     }
-    return lora_fits(M, columns) ? FP6_OK : FP6_ERR_SHAPE;
+    return lora_fits(M, columns, adapters) ? FP6_OK : FP6_ERR_SHAPE;
 }
 
 static int lora_any(int type, int64_t M, const fp6_lora_problem* pr, int count, int64_t adapters, const int32_t* index,

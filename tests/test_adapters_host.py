@@ -119,6 +119,10 @@ def test_workspaces_are_functions_of_the_sizes():
     two = P.fp6_lora_group_workspace_bytes(16, [(4096, 4096, 16), (1024, 4096, 16)], 4)
     assert two > P.fp6_lora_workspace_bytes(16, 4096, 4096, 16, 4)
     assert P.fp6_lora_workspace_bytes(0, 64, 64, 8) == 0 and P.fp6_lora_workspace_bytes(1, 64, 64, 9) == 0
+    # more workgroups than a launch counts: refused before anything is launched
+    assert P.fp6_lora_workspace_bytes(64, 1 << 22, 64, 8, 16) > 0 and P.fp6_lora_workspace_bytes(64, 1 << 24, 64, 8, 16) == 0
+    assert P.fp6_lora_workspace_bytes(256, 1 << 24, 64, 8, 4) == 0 and P.fp6_lora_workspace_bytes(1 << 20, 1 << 18, 64, 8, 4) == 0
+    assert P.fp6_lora_backward_workspace_bytes(64, 64, 16448, 8, 65535) == 0 and P.fp6_lora_backward_workspace_bytes(64, 64, 8192, 8, 65535) > 0
     assert P.fp6_lora_backward_workspace_bytes(1, 64, 65, 8) == 0 and P.fp6_linear_grad_workspace_bytes(1, 64, 64, format=1) == 0
 
 
@@ -148,7 +152,9 @@ def test_plan_counts_items_and_takes_neighbours(bits):
     for count in (1, 255, 4096, 4097, 0, 12288):
         t, at = _tensor(at, count, bits)
         tensors.append(t)
-    assert _plan(tensors, bits) == (0, 1 + 1 + 1 + 2 + 0 + 3)
+    assert _plan(tensors, bits) == (0, 1 + 1 + 4 + 5 + 0 + 12)                # few elements: 1024 to a workgroup
+    many, at = _tensor(at, 5000 * 1024 + 1, bits)
+    assert _plan(tensors + [many], bits) == (0, 1 + 1 + 1 + 2 + 0 + 3 + 1251)  # many: 4096
 
 
 def test_plan_refusals():
