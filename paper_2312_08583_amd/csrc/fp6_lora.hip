@@ -87,6 +87,24 @@ __device__ __forceinline__ void loads_are_issued()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// Sixteen rows of 128 bytes as the matrix cores take them: lane l has of row l % 16 the 16-byte pieces l / 16 (a) and 4 + l / 16 (b).  Read or written that
+// way an access is half a line of every row; here a and b are exchanged with what goes to and comes from memory in whole lines, eight rows an
+// access: a the rows 0 to 7 and b the rows 8 to 15, lane l the row l % 8 and the piece l / 16 + 4 * (l % 16 / 8).  Its own inverse.  All lanes call it.
+__device__ __forceinline__ void deal_lines(u32x4& a, u32x4& b)
+{
+    constexpr int kByEight = 0x128;      // each lane gets that of the lane eight away among its sixteen
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const int x = (int)a[e], y = (int)b[e];
+        a[e] = (uint32_t)__builtin_amdgcn_update_dpp(x, y, kByEight, 0xF, 0xC, false);
+        b[e] = (uint32_t)__builtin_amdgcn_update_dpp(y, x, kByEight, 0xF, 0x3, false);
+    }
+}
+
+// Every load is waited for here: for the end of a branch that loads.  Behind it the compiler would have to wait for all loads, those in flight for
+// later among them, whichever way was taken.
+__device__ __forceinline__ void loads_are_here() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
 // ------------------------------------------------------------------ shrink
 struct ShrinkLayer {
     const uint16_t* Q;      // [M, C]
@@ -349,8 +367,9 @@ constexpr int kExpandLds = TURNED ? 4 * 32 * kExpandLd * 2 : 16;
 // pieces of eight consecutive columns of each 64 (the rows of the W operand are dealt out so that it does).  P is two 16-bit terms
 // times a power of two per row.  PACKED (rank <= 16): both terms share one MFMA of contraction 32.  W stays in registers from row
 // tile to row tile as long as the adapter is the same.  SLICED (few rows): the terms are made here from the slices.
-// Bound by Y: 2048 x 8192 rank 16 18.7 us, rank 64 24 (as much again of the terms and of W out of L2) for 67 MB; a pass over Y alone takes 12.6 in
-// these half lines of 16 rows, 10.4 in whole ones.
+// Bound by Y: 2048 x 8192 rank 16 16.3 us, rank 64 21.6 (as much again of the terms and of W out of L2) for 67 MB; a pass over Y alone takes 10.4, in half
+// lines of 16 rows 12.6.  (With half lines, the loads of a tile past the end repeated, and prefetched loads waited for wherever W or the scaling
+// might have been loaded: 18.7 and 24.)
 template <int FMT, int JS, bool PACKED, bool TURNED, bool SLICED, int CB>
 __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, int slot, unsigned char* shared)
 {
@@ -391,29 +410,52 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
                 *reinterpret_cast<u32x4*>(to + 64 * c + 32) = b.y[c][1];
             }
     };
+    // many rows: Y in whole lines
+    const int line_row = i & 7, line_col = n0 + 8 * (g + 4 * (i >> 3));
+    auto load_lines = [&](Rows& b, int64_t t) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint16_t* y = L.Y + (size_t)(t < tiles ? min((tile0 + t) * 16 + 8 * h + line_row, args.M - 1) : 0) * D + line_col;
+#pragma unroll
+            for (int c = 0; c < CB; c++) b.y[c][h] = *reinterpret_cast<const u32x4*>(y + (n0 + 64 * c < D ? 64 * c : 0));
+        }
+    };
+    auto store_lines = [&](Rows& b, int64_t t, uint32_t rows) {
+#pragma unroll
+        for (int c = 0; c < CB; c++) deal_lines(b.y[c][0], b.y[c][1]);
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            if ((rows >> (8 * h + line_row)) & 1) {
+                uint16_t* to = L.out + (size_t)((tile0 + t) * 16 + 8 * h + line_row) * D + line_col;
+#pragma unroll
+                for (int c = 0; c < CB; c++)
+                    if (n0 + 64 * c < D) *reinterpret_cast<u32x4*>(to + 64 * c) = b.y[c][h];
+            }
+    };
     auto load = [&](Rows& b, int64_t t) {
-        const int64_t row = (tile0 + t) * 16 + i;
+        const int64_t row = SLICED || t < tiles ? (tile0 + t) * 16 + i : 0;
         b.word = owner_word(args.index, row, args.M);
         const int64_t near = min(row, args.M - 1);
         if (!SLICED) {
-            load_y(b, near);
+            load_lines(b, t);
             const uint16_t* p = L.terms + (size_t)near * 2 * rank;
             b.power = FMT != kE3M2B ? L.P[near] : 1.0f;
 #pragma unroll
             for (int s = 0; s < JS; s++)
 #pragma unroll
                 for (int k = 0; k < TERMS; k++) {
-                    const int j0 = 32 * s + 8 * g, most = PACKED ? 2 * rank : rank;
-                    const u32x4 v = *reinterpret_cast<const u32x4*>(p + k * rank + min(j0, most - 8));
-                    b.p[s][k] = j0 < most ? v : u32x4{0, 0, 0, 0};
+                    // (past the rank: `work` puts zeros in its place)
+                    b.p[s][k] = *reinterpret_cast<const u32x4*>(p + k * rank + min(32 * s + 8 * g, (PACKED ? 2 * rank : rank) - 8));
                 }
         }
     };
 
     int held = kNoAdapter;               // the adapter whose operands are in w
+    float scale = 1.0f;                  // and its scaling
     u32x4 w[CB][4][JS];
     auto hold = [&](int a) {
         held = a;
+        if (!SLICED && args.scaling) scale = args.scaling[a];
         const uint16_t* W = L.W + (size_t)a * rank * D;
 #pragma unroll
         for (int s = 0; s < JS; s++) {
@@ -456,6 +498,7 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
                 }
             }
         }
+        if (!SLICED) loads_are_here();
     };
 
     auto work = [&](Rows& b, int64_t t) {
@@ -463,7 +506,12 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
         const int64_t row = t < tiles ? (tile0 + t) * 16 + i : args.M;
         b.mine = owner_of(b.word, row, args.M, args.adapters);
         uint64_t pending = __ballot(b.mine != kNoAdapter) & 0xFFFF;
-        bool store = !SLICED && b.mine == kNoAdapter && slot == 0 && row < args.M && L.out != L.Y;
+        // (rows to be written: those of an adapter, and where Y lies elsewhere those without one)
+        const uint32_t write = SLICED ? 0 : (uint32_t)__ballot(row < args.M && (b.mine != kNoAdapter || L.out != L.Y)) & 0xFFFF;
+        if (!SLICED) {
+#pragma unroll
+            for (int c = 0; c < CB; c++) deal_lines(b.y[c][0], b.y[c][1]);
+        }
         if (SLICED && b.mine == kNoAdapter && slot == 0 && row < args.M && L.out != L.Y) {
             // (few rows: Y is read for the adapter at hand, these are copied by themselves)
             const u32x4* from = reinterpret_cast<const u32x4*>(L.Y + (size_t)row * D + n0 + 8 * g);
@@ -548,8 +596,16 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
                     }
                 }
             }
-            if (!SLICED && a != held) hold(a);
-            const float scale = args.scaling ? args.scaling[a] : 1.0f;
+            if (SLICED) {
+                scale = args.scaling ? args.scaling[a] : 1.0f;
+            } else {
+                if (a != held) hold(a);
+#pragma unroll
+                for (int s = 0; s < JS; s++)
+#pragma unroll
+                    for (int k = 0; k < TERMS; k++)
+                        if (32 * s + 8 * g >= (PACKED ? 2 * rank : rank)) b.p[s][k] = u32x4{0, 0, 0, 0};
+            }
 #pragma unroll
             for (int c = 0; c < CB; c++) {
                 float4v acc[4] = {float4v{0, 0, 0, 0}, float4v{0, 0, 0, 0}, float4v{0, 0, 0, 0}, float4v{0, 0, 0, 0}};
@@ -570,12 +626,11 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
                             const float hi = to_float<FMT>((uint16_t)(d >> 16)) + acc[t4][2 * p + 1] * b.power * scale;
                             b.y[c][t4 >> 1][2 * (t4 & 1) + p] = to_bits<FMT>(lo) | (uint32_t)to_bits<FMT>(hi) << 16;
                         }
-                    store = true;
                 }
             }
             if (SLICED && b.mine == a) store_y(b, row);
         }
-        if (!SLICED && store) store_y(b, row);
+        if (write) store_lines(b, t, write);
     };
 
     if (SLICED) {
@@ -585,16 +640,16 @@ __device__ __forceinline__ void expand_block(const ExpandArgs& args, int block, 
             work(b, t);
         }
     } else {
-        // the next row tile is in flight while one is worked on (past the end: the last one again, not stored)
+        // the next row tile is in flight while one is worked on (past the end: all lanes read row 0, which costs little, and nothing is done)
         Rows b[2];
         load(b[0], 0);
         if (args.adapters == 1) hold(0);
         loads_are_issued();
         for (int64_t t = 0; t < tiles; t += 2) {
-            load(b[1], min(t + 1, tiles - 1));
+            load(b[1], t + 1);
             loads_are_issued();
             work(b[0], t);
-            load(b[0], min(t + 2, tiles - 1));
+            load(b[0], t + 2);
             loads_are_issued();
             work(b[1], t + 1);
         }
@@ -941,12 +996,12 @@ union SecondLds {
     OuterLds<FMT, JT, CT> outer;
 };
 
-// the gradient of A, and dX: 4096 x 8192 rank 16 56 us for 201 MB, 3.6 TB/s
+// the gradient of A, and dX: 4096 x 8192 rank 16 49 us for 201 MB, 4.1 TB/s
 template <int FMT, int JT, int CT, bool SLICED>
 __global__ __launch_bounds__(256) void lora_second_kernel(ExpandArgs expand, int expands, OuterArgs outer)
 {
     __shared__ __align__(16) SecondLds<FMT, JT, CT> lds;
-    // (in turn, a workgroup of the one beside one of the other, they take longer: 56 us become 59, at rank 128 120 become 157)
+    // (in turn, a workgroup of the one beside one of the other, they took longer: 56 us became 59, at rank 128 120 became 157)
     const int blocks = (outer.C + 64 * CT - 1) / (64 * CT) * outer.splits, outers = blocks * outer.adapters, id = (int)blockIdx.x;
     if (id < outers) outer_block<FMT, JT, CT, false, false>(outer, id % blocks, id / blocks, lds.outer);
     else expand_block<FMT, JT <= 2 ? 1 : JT / 2, JT == 1, true, SLICED, SLICED || JT == 8 ? 1 : 2>(expand, (id - outers) % expands, (id - outers) / expands, lds.expand);
