@@ -482,6 +482,8 @@ int fp6_linear_grad(int format, const uint16_t *dY, int64_t M, const void *hi_t,
  *     smallest such power that brings the block to 448 or below; all bytes zero is the state zero.  The last kept bit is
  *     rounded up with the probability that makes the rounding unbiased, by a hash of the element's number, t and `seed` (the
  *     numbers run through the tensors of the plan, each starting at a multiple of 256); a nonzero sqrt(v) never becomes zero.
+ *     The smallest code is 2^-17 to 2^-18 of the block's largest number.  A state that is not finite, as that of a gradient whose
+ *     square overflows, becomes NaN: its element is lost from the next call on, its block's scale is that of the others.
  *   grad_type FP6_F32, FP6_F16 or FP6_BF16; copy_type FP6_F16, FP6_BF16 or FP6_NO_COPY: one of each for all tensors of a plan.
  *   step      int32 on the device, the steps done so far; the call adds one.
  * fp6_adamw_plan writes, on the host, what the kernel needs of the tensors into plan_host (fp6_adamw_plan_bytes bytes); the

@@ -34,6 +34,15 @@ __device__ __forceinline__ int block_exponent(float top)
     return top > 0.0f ? max(e, -126) : -127;
 }
 
+// The larger magnitude, of those that are finite: an infinity is its own element's loss, and no scale for the others of its block (with its
+// exponent they became 0, their u 2^111, whose square overflows in the next call: 256 parameters were NaN in the third).  Finite u are below
+// 2^64, so e of a block of u is 56 at most, and the least code that its others get, 2^47, has a finite square.
+__device__ __forceinline__ float largest(float top, float x)
+{
+    const float a = fabsf(x);
+    return a < __builtin_inff() ? fmaxf(top, a) : top;
+}
+
 // x * 2^-e to an e4m3 code; `noise` in 0 .. 65535 decides between the neighbours; `least`: the smallest code that a nonzero x may get.
 // y in units of its last kept bit (2^-9 below 2^-6) plus the noise's fraction, cut: a product by a power of two and one addition, as the
 // definition has it.  An infinity or NaN becomes NaN.
@@ -191,8 +200,8 @@ __device__ __forceinline__ void step_block(const AdamwItem& it, int block, int l
 #pragma unroll
         for (int e = 0; e < 4; e++)
             if (WHOLE || e < n) {
-                tm = fmaxf(tm, fabsf(m[e]));
-                tu = fmaxf(tu, u[e]);
+                tm = largest(tm, m[e]);
+                tu = largest(tu, u[e]);
             }
         const int em = block_exponent(wave_max(tm)), eu = block_exponent(wave_max(tu));
         const float dm = two_to(-em), du = two_to(-eu);
