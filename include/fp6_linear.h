@@ -490,7 +490,7 @@ int fp6_linear_grad(int format, const uint16_t *dY, int64_t M, const void *hi_t,
  * caller copies it to 16-byte aligned device memory once and keeps it as long as the tensors stay where they are.  It refuses
  * NULL (FP6_ERR_NULL), misaligned (16 bytes; scale bytes: any; FP6_ERR_ALIGN) and overlapping (FP6_ERR_OVERLAP: what is
  * written twice, or written and read as a gradient) tensors; a count of 0 is fine.  `items` receives what fp6_adamw wants to know.
- * One call at a time may use a plan; a plan of other state_bits than the call says, or what is no plan: nothing is changed.
+ * One call at a time may use a plan; a plan of other state_bits or types than the call says, or what is no plan: nothing is changed.
  * lr may come from the device (lr_device != NULL: it counts instead of lr), as may grad_scale (NULL: 1; the inverse of a loss
  * scale, a clipping factor); found_inf (NULL: never): where it is not 0 the call changes nothing, not even step.  So a captured
  * call can be replayed as step, learning rate and scale move on.

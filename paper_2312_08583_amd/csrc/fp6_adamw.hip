@@ -72,6 +72,12 @@ __device__ __forceinline__ float grad_of(_Float16 g) { return (float)g; }
 template <>
 __device__ __forceinline__ float grad_of(__bf16 g) { return (float)g; }
 
+template <typename T>
+constexpr int type_of()
+{
+    return __is_same(T, float) ? FP6_F32 : (__is_same(T, __bf16) ? FP6_BF16 : FP6_F16);
+}
+
 struct StepScalars {
     float decay, first, second, b1, c1, b2, c2, eps, scale;
     uint32_t salt;
@@ -244,8 +250,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwHeader* __restrict__ pl
     StepScalars s;
     const uint32_t t = (uint32_t)*step + 1;
     if (call.found_inf && *call.found_inf != 0.0f) return;
-    // (not a plan, one of the other kind, or fewer items than the caller says: nothing beyond it is touched)
-    if (plan->magic != kAdamwMagic || plan->state_bits != BITS) return;
+    // (not a plan, one of another kind, or fewer items than the caller says: nothing beyond it is touched)
+    if (plan->magic != kAdamwMagic || plan->kind != adamw_kind(BITS, type_of<G>(), sizeof(C) == 2 ? type_of<C>() : FP6_NO_COPY)) return;
     items = min(items, (int64_t)plan->items);
     s.scale = call.grad_scale ? *call.grad_scale : 1.0f;
     const double lr = call.lr_device ? (double)*call.lr_device : call.lr;

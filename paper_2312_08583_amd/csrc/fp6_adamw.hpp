@@ -15,9 +15,15 @@ constexpr int64_t adamw_item(int64_t elements) { return elements <= (int64_t)4 <
 // address follow one another at 13 ns, and 2048 of them alone took 27 us.
 constexpr int kArrivalGroups = 64;
 
+// What the addresses of a plan were worked out with: a call of another kind would read and write beside its tensors.
+constexpr uint32_t adamw_kind(int state_bits, int grad_type, int copy_type)
+{
+    return (uint32_t)state_bits | (uint32_t)grad_type << 8 | (uint32_t)(copy_type & 0xFF) << 16;
+}
+
 // [header][items]
 struct AdamwHeader {
-    uint32_t magic, state_bits;
+    uint32_t magic, kind;
     uint64_t items;
     uint32_t unused[28];
     struct {

@@ -200,7 +200,7 @@ static int adamw_plan(const fp6_adamw_tensor* t, int64_t count, int state_bits, 
     unsigned char* at = (unsigned char*)plan_host;
     AdamwHeader h{};
     h.magic = kAdamwMagic;
-    h.state_bits = (uint32_t)state_bits;
+    h.kind = adamw_kind(state_bits, grad_type, copy_type);
     h.items = (uint64_t)l.items;
     std::memcpy(at, &h, sizeof h);
     at += sizeof h;
