@@ -511,6 +511,7 @@ def fp6_linear_group(layers, outs=None, workspace: Optional[torch.Tensor] = None
     ys = _native_group(layers, outs, workspace)
     if ys is not None:
         return ys
+    layers = [tuple(layer) for layer in layers]          # (holds the tensors, whatever other threads do to the list)
     arr, M, ys = _group_array(layers, outs=outs)
     need = int(lib().fp6_linear_group_workspace_bytes(M, arr, len(layers)))
     if workspace is None:
@@ -728,6 +729,7 @@ def fp6_lora_group(layers, index: Optional[torch.Tensor] = None, scaling: Option
     done = _native["lora_group"](layers, index, scaling, outs, workspace)
     if done is not None:
         return done
+    layers = [tuple(layer) for layer in layers]          # (holds the tensors, whatever other threads do to the list)
     if not 1 <= len(layers) <= FP6_GROUP_MAX:
         raise Fp6Error("a group holds 1 to %d projections" % FP6_GROUP_MAX)
     if outs is not None and len(outs) != len(layers):

@@ -162,6 +162,26 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t count)
     return PyObject_CallFunction(fail, "is", status, kNames[kind]);
 }
 
+// The tensors of a list's items, held while other threads may run and change the list: their memory would be given to others before the launch.
+class Held {
+    PyObject* p[4 * FP6_GROUP_MAX];
+    int count = 0;
+
+public:
+    Held() = default;
+    Held(const Held&) = delete;
+    Held& operator=(const Held&) = delete;
+    ~Held()
+    {
+        while (count) Py_DECREF(p[--count]);
+    }
+    void add(PyObject* o)
+    {
+        Py_INCREF(o);
+        p[count++] = o;
+    }
+};
+
 // group(layers, outs, workspace) -> list of Y, or None
 PyObject* group(PyObject*, PyObject* const* a, Py_ssize_t count)
 {
@@ -172,6 +192,7 @@ PyObject* group(PyObject*, PyObject* const* a, Py_ssize_t count)
     if (n < 1 || n > FP6_GROUP_MAX || PySequence_Fast_GET_SIZE(a[1]) < n) Py_RETURN_NONE;
     fp6_linear_problem problems[FP6_GROUP_MAX];
     PyObject* ys[FP6_GROUP_MAX];
+    Held held;
     int status = FP6_OK;
     try {
         int64_t M = 0;
@@ -184,6 +205,7 @@ PyObject* group(PyObject*, PyObject* const* a, Py_ssize_t count)
             if (!read_layer(f[0], f[1], f[2], f[3], f[4], f[5], 0, 4, c10::kHalf, &l) || (i && l.M != M) || !read_out(ys[i], c10::kHalf, &l))
                 Py_RETURN_NONE;
             M = l.M;
+            for (int k = 0; k < 4; k++) held.add(f[k]);
             problems[i] = fp6_linear_problem{(const uint16_t*)l.x, l.hi, l.lo, (const uint16_t*)l.scales, l.N, l.K, (uint16_t*)l.y};
         }
         const at::Tensor* ws = nullptr;
@@ -196,7 +218,7 @@ PyObject* group(PyObject*, PyObject* const* a, Py_ssize_t count)
         void* w = ws ? ws->data_ptr() : nullptr;
         const size_t bytes = ws ? (size_t)ws->numel() : 0;
         void* stream = c10::hip::getCurrentHIPStream().stream();
-        for (Py_ssize_t i = 0; i < n; i++) Py_INCREF(ys[i]);          // (the lists may change while other threads run)
+        for (Py_ssize_t i = 0; i < n; i++) Py_INCREF(ys[i]);
         Py_BEGIN_ALLOW_THREADS
         status = call_group(M, problems, (int)n, w, bytes, stream);
         Py_END_ALLOW_THREADS
@@ -372,6 +394,7 @@ PyObject* lora_group(PyObject*, PyObject* const* a, Py_ssize_t count)
     if (n < 1 || n > FP6_GROUP_MAX || (a[3] != Py_None && PySequence_Fast_GET_SIZE(a[3]) != n)) Py_RETURN_NONE;
     fp6_lora_problem problems[FP6_GROUP_MAX];
     PyObject* results[FP6_GROUP_MAX];
+    Held held;
     int status = FP6_OK;
     try {
         Checked c;
@@ -387,12 +410,13 @@ PyObject* lora_group(PyObject*, PyObject* const* a, Py_ssize_t count)
             if (i == 0) first = r;
             if (r.M != first.M || r.adapters != first.adapters || r.type != first.type) Py_RETURN_NONE;
             results[i] = out == Py_None ? f[3] : out;
+            for (int k = 0; k < 4; k++) held.add(f[k]);
         }
         const int32_t* index = (const int32_t*)c.optional(a[1], c10::kInt, {first.M});
         const float* scaling = (const float*)c.optional(a[2], c10::kFloat, {first.adapters});
         if (!read_workspace(c, a[4], &ws, &bytes)) Py_RETURN_NONE;
         void* stream = c10::hip::getCurrentHIPStream().stream();
-        for (Py_ssize_t i = 0; i < n; i++) Py_INCREF(results[i]);          // (the lists may change while other threads run)
+        for (Py_ssize_t i = 0; i < n; i++) Py_INCREF(results[i]);
         Py_BEGIN_ALLOW_THREADS
         status = call_lora_group(type_of(first.type), first.M, problems, (int)n, first.adapters, index, scaling, ws, bytes, stream);
         Py_END_ALLOW_THREADS
