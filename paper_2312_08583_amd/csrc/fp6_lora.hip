@@ -1101,21 +1101,30 @@ static OuterPlan plan_outer(int64_t M, int C, int rank, int adapters, bool fused
 // The gradient of B and the shrink of dY in one reading of dY: the shrink's parts, one per 256 columns, cost rank / 64 of what they save.
 static bool fuses(int64_t M, int rank) { return M > kFewRows && rank <= 32; }
 
+// (turned: ranks above 32 only, which is where dY is not read for dB and dS together, and up to kFewRows the shrink shares a launch)
 template <int FMT, bool TURNED>
 static hipError_t launch_shrink(const ShrinkArgs& a, bool narrow, int64_t workgroups, hipStream_t stream)
 {
     int rank = 0;
     for (int l = 0; l < a.layers; l++) rank = a.layer[l].rank > rank ? a.layer[l].rank : rank;
     const dim3 grid((unsigned)workgroups, (unsigned)a.slots), block(256);
-    if (narrow) {
-        if (rank <= 16) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 1, TURNED>), grid, dim3(64 * kShrinkWaves<1, 1>), 0, stream, a);
-        else if (rank <= 32) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 1, TURNED>), grid, dim3(64 * kShrinkWaves<2, 1>), 0, stream, a);
-        else if (rank <= 64) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, 1, TURNED>), grid, dim3(64 * kShrinkWaves<4, 1>), 0, stream, a);
-        else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 8, 1, TURNED>), grid, dim3(64 * kShrinkWaves<8, 1>), 0, stream, a);
+    if constexpr (!TURNED) {
+        if (rank <= 16) {
+            if (narrow) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 1, TURNED>), grid, dim3(64 * kShrinkWaves<1, 1>), 0, stream, a);
+            else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 4, TURNED>), grid, block, 0, stream, a);
+            return hipGetLastError();
+        }
+        if (rank <= 32) {
+            if (narrow) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 1, TURNED>), grid, dim3(64 * kShrinkWaves<2, 1>), 0, stream, a);
+            else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 4, TURNED>), grid, block, 0, stream, a);
+            return hipGetLastError();
+        }
+    }
+    if (rank <= 64) {
+        if (narrow) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, 1, TURNED>), grid, dim3(64 * kShrinkWaves<4, 1>), 0, stream, a);
+        else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, 4, TURNED>), grid, block, 0, stream, a);
     } else {
-        if (rank <= 16) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 1, 4, TURNED>), grid, block, 0, stream, a);
-        else if (rank <= 32) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 2, 4, TURNED>), grid, block, 0, stream, a);
-        else if (rank <= 64) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 4, 4, TURNED>), grid, block, 0, stream, a);
+        if (narrow) hipLaunchKernelGGL((lora_shrink_kernel<FMT, 8, 1, TURNED>), grid, dim3(64 * kShrinkWaves<8, 1>), 0, stream, a);
         else hipLaunchKernelGGL((lora_shrink_kernel<FMT, 8, 2, TURNED>), grid, block, 0, stream, a);
     }
     return hipGetLastError();
@@ -1156,28 +1165,42 @@ static hipError_t launch_expand(const ExpandArgs& a, bool few, int rank, int64_t
     return hipGetLastError();
 }
 
+// 64 * CT columns a workgroup: 256 for ranks up to 64 only.  By column (the gradient of B): ranks above 32, the others' shares dY's reading with the shrink or,
+// up to kFewRows, its launch.
 template <int FMT, int CT, bool BY_COLUMN>
-static void launch_outer_rank(const OuterArgs& a, dim3 grid, hipStream_t stream)
+static hipError_t launch_outer_rank(const OuterArgs& a, dim3 grid, hipStream_t stream)
 {
-    if (a.rank <= 16) hipLaunchKernelGGL((lora_outer_kernel<FMT, 1, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
-    else if (a.rank <= 32) hipLaunchKernelGGL((lora_outer_kernel<FMT, 2, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
-    else if (a.rank <= 64) hipLaunchKernelGGL((lora_outer_kernel<FMT, 4, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((lora_outer_kernel<FMT, 8, 2, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
+    if constexpr (!BY_COLUMN) {
+        if (a.rank <= 16) {
+            hipLaunchKernelGGL((lora_outer_kernel<FMT, 1, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
+            return hipGetLastError();
+        }
+        if (a.rank <= 32) {
+            hipLaunchKernelGGL((lora_outer_kernel<FMT, 2, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
+            return hipGetLastError();
+        }
+    }
+    if (a.rank <= 64) {
+        hipLaunchKernelGGL((lora_outer_kernel<FMT, 4, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
+    } else {
+        if constexpr (CT == 2) hipLaunchKernelGGL((lora_outer_kernel<FMT, 8, CT, BY_COLUMN, false>), grid, dim3(256), 0, stream, a);
+        else return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
 }
 
 template <int FMT, bool BY_COLUMN>
 static hipError_t launch_outer(const OuterArgs& a, int columns, hipStream_t stream)
 {
     const dim3 grid((unsigned)(ceil_div(a.C, columns) * a.splits), (unsigned)a.adapters);
-    if (a.S) {
-        if (a.rank <= 16) hipLaunchKernelGGL((lora_outer_kernel<FMT, 1, 4, true, true>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((lora_outer_kernel<FMT, 2, 4, true, true>), grid, dim3(256), 0, stream, a);
-    } else if (columns == 128) {
-        launch_outer_rank<FMT, 2, BY_COLUMN>(a, grid, stream);
-    } else {
-        launch_outer_rank<FMT, 4, BY_COLUMN>(a, grid, stream);
+    if constexpr (BY_COLUMN) {
+        if (a.S) {
+            if (a.rank <= 16) hipLaunchKernelGGL((lora_outer_kernel<FMT, 1, 4, true, true>), grid, dim3(256), 0, stream, a);
+            else hipLaunchKernelGGL((lora_outer_kernel<FMT, 2, 4, true, true>), grid, dim3(256), 0, stream, a);
+            return hipGetLastError();
+        }
     }
-    return hipGetLastError();
+    return columns == 128 ? launch_outer_rank<FMT, 2, BY_COLUMN>(a, grid, stream) : launch_outer_rank<FMT, 4, BY_COLUMN>(a, grid, stream);
 }
 
 template <int FMT>
@@ -1198,7 +1221,8 @@ static hipError_t launch_second_rank(const ExpandArgs& e, int expands, const Out
     if (o.rank <= 16) hipLaunchKernelGGL((lora_second_kernel<FMT, 1, CT, SLICED>), grid, block, 0, stream, e, expands, o);
     else if (o.rank <= 32) hipLaunchKernelGGL((lora_second_kernel<FMT, 2, CT, SLICED>), grid, block, 0, stream, e, expands, o);
     else if (o.rank <= 64) hipLaunchKernelGGL((lora_second_kernel<FMT, 4, CT, SLICED>), grid, block, 0, stream, e, expands, o);
-    else hipLaunchKernelGGL((lora_second_kernel<FMT, 8, 2, SLICED>), grid, block, 0, stream, e, expands, o);
+    else if constexpr (CT == 2) hipLaunchKernelGGL((lora_second_kernel<FMT, 8, CT, SLICED>), grid, block, 0, stream, e, expands, o);
+    else return hipErrorInvalidValue;          // (the grid counts columns by 256, which ranks above 64 do not take)
     return hipGetLastError();
 }
 
