@@ -680,8 +680,20 @@ struct OuterArgs {
 
 constexpr int kChunk = 64;      // rows between two barriers (a lane of a wavefront each)
 
-template <int FMT, int JT, int CT>
-struct OuterLds {
+// (FUSED and rank above 16: W's operands, 64 registers of every lane otherwise, with which a second workgroup would not fit the compute unit)
+template <int JT, int CT, bool FUSED>
+struct OuterW {
+    u32x4 w[JT][2 * CT][64];
+};
+template <int CT, bool FUSED>
+struct OuterW<1, CT, FUSED> {};
+template <int JT, int CT>
+struct OuterW<JT, CT, false> {};
+template <int CT>
+struct OuterW<1, CT, false> {};
+
+template <int FMT, int JT, int CT, bool FUSED>
+struct OuterLds : OuterW<JT, CT, FUSED> {
     static constexpr int TERMS = FMT == kE3M2B ? 3 : 2, kCols = 64 * CT, kLdQ = kCols + 16, kLdP = kChunk + 8;
     uint16_t q[kChunk * kLdQ];
     uint16_t p[TERMS][16 * JT][kLdP];
@@ -699,9 +711,9 @@ struct OuterLds {
 // FUSED: the chunk of Q in LDS is multiplied with W as well, S[block][m][j] = s * sum over the block's columns of Q[m][c] W[a][c][j]: the part of
 // a shrink that this block of columns has, so that Q is read once for both.
 template <int FMT, int JT, int CT, bool BY_COLUMN, bool FUSED>
-__device__ __forceinline__ void outer_block(const OuterArgs& args, int block, int a, OuterLds<FMT, JT, CT>& lds)
+__device__ __forceinline__ void outer_block(const OuterArgs& args, int block, int a, OuterLds<FMT, JT, CT, FUSED>& lds)
 {
-    using Lds = OuterLds<FMT, JT, CT>;
+    using Lds = OuterLds<FMT, JT, CT, FUSED>;
     constexpr int TERMS = Lds::TERMS, kCols = Lds::kCols, kLdQ = Lds::kLdQ;
     constexpr int kQv = kChunk * kCols / 8 / 256;                              // 16-byte pieces of Q a thread
     constexpr int kPv = JT;                                                    // float4 of P a thread
@@ -732,7 +744,8 @@ __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, in
 
     // FUSED: W of the block's columns as operands, turned in LDS (each wavefront multiplies 16 rows with all columns)
     constexpr int kSteps = FUSED ? kCols / 32 : 1, kLdW = 16 * JT + 8;
-    u32x4 w[FUSED ? JT : 1][kSteps];
+    constexpr bool kSharedW = FUSED && JT > 1;
+    u32x4 w[FUSED && !kSharedW ? JT : 1][kSharedW ? 1 : kSteps];
     if constexpr (FUSED) {
         static_assert(kCols * kLdW <= kChunk * kLdQ, "W of the columns fits where the chunk of Q lies");
         const int per = rank / 8, pieces = min(kCols, C - c0) * per;
@@ -740,16 +753,28 @@ __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, in
         for (int p = threadIdx.x; p < kCols * per; p += 256)
             *reinterpret_cast<u32x4*>(lds.q + (p / per) * kLdW + (p % per) * 8) = p < pieces ? from[p] : u32x4{0, 0, 0, 0};
         __syncthreads();
+        auto operand = [&](int j, int k) {
+            u32x4 v;
 #pragma unroll
-        for (int j = 0; j < JT; j++)
+            for (int e = 0; e < 2; e++) {
+                const u32x2 d = read_turned(lds.q + (32 * k + 8 * g + 4 * e + (i >> 2)) * kLdW + min(16 * j + 4 * (i & 3), rank - 4));
+                v[2 * e] = d[0];
+                v[2 * e + 1] = d[1];
+            }
+            return v;
+        };
+        if constexpr (kSharedW) {
 #pragma unroll
-            for (int k = 0; k < kSteps; k++)
+            for (int p = 0; p < JT * kSteps / 4; p++) {
+                const int at = wave + 4 * p;
+                lds.w[at / kSteps][at % kSteps][lane] = operand(at / kSteps, at % kSteps);
+            }
+        } else {
 #pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    const u32x2 d = read_turned(lds.q + (32 * k + 8 * g + 4 * e + (i >> 2)) * kLdW + min(16 * j + 4 * (i & 3), rank - 4));
-                    w[j][k][2 * e] = d[0];
-                    w[j][k][2 * e + 1] = d[1];
-                }
+            for (int j = 0; j < JT; j++)
+#pragma unroll
+                for (int k = 0; k < kSteps; k++) w[j][k] = operand(j, k);
+        }
     }
     // The rows of this adapter, 64 chunks at a time: one load a lane and chunk, all under way together.
     int batch = begin;
@@ -880,7 +905,7 @@ __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, in
         chunk = find(rows);
         if (chunk < end) load(chunk, rows);
         loads_are_issued();
-        if (FUSED) {
+        if constexpr (FUSED) {
             float4v d[JT];
 #pragma unroll
             for (int j = 0; j < JT; j++) d[j] = float4v{0, 0, 0, 0};
@@ -888,7 +913,12 @@ __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, in
             for (int k = 0; k < kSteps; k++) {
                 const half8 x = *reinterpret_cast<const half8*>(lds.q + (16 * wave + i) * kLdQ + 32 * k + 8 * g);
 #pragma unroll
-                for (int j = 0; j < JT; j++) d[j] = mfma16x16x32_of<FMT>(x, __builtin_bit_cast(half8, w[j][k]), d[j]);
+                for (int j = 0; j < JT; j++) {
+                    u32x4 v;
+                    if constexpr (kSharedW) v = lds.w[j][k][lane];
+                    else v = w[j][k];
+                    d[j] = mfma16x16x32_of<FMT>(x, __builtin_bit_cast(half8, v), d[j]);
+                }
             }
             float* S = args.S + ((size_t)(block % blocks) * args.M + m0) * rank;
 #pragma unroll
@@ -969,7 +999,7 @@ __device__ __forceinline__ void outer_block(const OuterArgs& args, int block, in
 template <int FMT, int JT, int CT, bool BY_COLUMN, bool FUSED>
 __global__ __launch_bounds__(256) void lora_outer_kernel(OuterArgs args)
 {
-    __shared__ __align__(16) OuterLds<FMT, JT, CT> lds;
+    __shared__ __align__(16) OuterLds<FMT, JT, CT, FUSED> lds;
     outer_block<FMT, JT, CT, BY_COLUMN, FUSED>(args, blockIdx.x, blockIdx.y, lds);
 }
 
@@ -979,7 +1009,7 @@ __global__ __launch_bounds__(256) void lora_outer_kernel(OuterArgs args)
 template <int FMT, int JT>
 union FirstLds {
     unsigned char shrink[kShrinkLds<JT, 1, true, 4>];
-    OuterLds<FMT, JT, 2> outer;
+    OuterLds<FMT, JT, 2, false> outer;
 };
 
 // few rows: dS, and the gradient of B
@@ -995,7 +1025,7 @@ __global__ __launch_bounds__(256) void lora_first_kernel(ShrinkArgs shrink, int 
 template <int FMT, int JT, int CT>
 union SecondLds {
     unsigned char expand[kExpandLds<true>];
-    OuterLds<FMT, JT, CT> outer;
+    OuterLds<FMT, JT, CT, false> outer;
 };
 
 // the gradient of A, and dX: 4096 x 8192 rank 16 49 us for 201 MB, 4.1 TB/s
@@ -1070,12 +1100,18 @@ static ShrinkPlan plan_shrink(int64_t M, int C, int rank, int adapters)
 
 static int expand_slots(int64_t M, const ShrinkPlan& p) { return M <= kSlotRows ? p.slots : 1; }
 
-// Columns of an outer workgroup, and ranges of rows that separate workgroups take.  Two workgroups fit a compute unit, 512 are a round (516 took
+// Columns of an outer workgroup, and ranges of rows that separate workgroups take.  Where two workgroups fit a compute unit 512 are a round (516 took
 // 70 us where 430 take 54: the last four had a round to themselves); a workgroup needs about 4 us beside its chunks and 3 (128 columns: 2.2) for each, adapters sharing
-// the rows evenly; every range costs a tensor of partial sums, written and read at 4 TB/s, and together they cost a launch.
+// the rows in runs (in mixed order each of them reads every chunk that has a row of its own, and the same plan takes longer: gradients of 2048 x 8192 x 8192, rank 16,
+// four adapters 64 us in runs, 90 mixed); every range costs a tensor of partial sums, written and read at 4 TB/s, and together they cost a launch.
 struct OuterPlan {
     int columns, splits;
 };
+
+// Workgroups of an outer product that a compute unit holds at a time, by their registers: two where a wavefront has 256 of a SIMD's 512 at most, as up to
+// rank 64, one above (2048 x 8192 x 8192, rank 128: 203 us, counted as two 223).  Ranks above 32 with 256 columns count as two although fp16, and dA beside
+// dX in bf16, have one: counted as one they get 128 columns, which read P twice as often (4096 x 22016 x 8192, rank 64: 276 and 207 us became 282 and 245).
+static int outer_resident(int rank) { return rank > 64 ? 1 : 2; }
 
 static OuterPlan plan_outer(int64_t M, int C, int rank, int adapters, bool fused)
 {
@@ -1088,7 +1124,7 @@ static OuterPlan plan_outer(int64_t M, int C, int rank, int adapters, bool fused
         for (int splits = 1; splits <= 64 && splits <= chunks; splits++) {
             const double chunk = columns == 256 ? 3.0 : 2.2, mine = (double)ceil_div(chunks, (int64_t)splits * adapters);
             const double partial = splits > 1 ? 4.0 + 8e-6 * splits * adapters * rank * C / 4 : 0.0;
-            const double cost = (double)ceil_div(have * splits, 512) * (4.0 + chunk * mine) + partial;
+            const double cost = (double)ceil_div(have * splits, 256 * outer_resident(rank)) * (4.0 + chunk * mine) + partial;
             if (cost < least) {
                 least = cost;
                 best = OuterPlan{columns, splits};
