@@ -34,15 +34,6 @@ __device__ __forceinline__ int block_exponent(float top)
     return top > 0.0f ? max(e, -126) : -127;
 }
 
-// The larger magnitude, of those that are finite: an infinity is its own element's loss, and no scale for the others of its block (with its
-// exponent they became 0, their u 2^111, whose square overflows in the next call: 256 parameters were NaN in the third).  Finite u are below
-// 2^64, so e of a block of u is 56 at most, and the least code that its others get, 2^47, has a finite square.
-__device__ __forceinline__ float largest(float top, float x)
-{
-    const float a = fabsf(x);
-    return a < __builtin_inff() ? fmaxf(top, a) : top;
-}
-
 // x * 2^-e to an e4m3 code; `noise` in 0 .. 65535 decides between the neighbours; `least`: the smallest code that a nonzero x may get.
 // y in units of its last kept bit (2^-9 below 2^-6) plus the noise's fraction, cut: a product by a power of two and one addition, as the
 // definition has it.  An infinity or NaN becomes NaN.
@@ -61,6 +52,30 @@ __device__ __forceinline__ float wave_max(float v)
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
     return v;
+}
+
+// The largest magnitude of a block, of those that are finite: an infinity is its own element's loss, and no scale for the others of its block (with its
+// exponent they became 0, their u 2^111, whose square overflows in the next call: 256 parameters were NaN in the third).  Finite u are below
+// 2^64, so e of a block of u is 56 at most, and the least code that its others get, 2^47, has a finite square.  (Infinities are sought where the
+// maximum is one: 109 million elements 396.5 us, 399.9 with a look at every element and 394.3 with none.)
+template <bool WHOLE>
+__device__ __forceinline__ float block_top(const float (&x)[4], int n)
+{
+    float top = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        if (WHOLE || e < n) top = fmaxf(top, fabsf(x[e]));
+    top = wave_max(top);
+    if (top == __builtin_inff()) {
+        top = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const float a = fabsf(x[e]);
+            if ((WHOLE || e < n) && a < __builtin_inff()) top = fmaxf(top, a);
+        }
+        top = wave_max(top);
+    }
+    return top;
 }
 
 template <typename T>
@@ -202,14 +217,7 @@ __device__ __forceinline__ void step_block(const AdamwItem& it, int block, int l
         store4<WHOLE>((float*)it.first + at, n, m);
         store4<WHOLE>((float*)it.second + at, n, v);
     } else {
-        float tm = 0.0f, tu = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 4; e++)
-            if (WHOLE || e < n) {
-                tm = largest(tm, m[e]);
-                tu = largest(tu, u[e]);
-            }
-        const int em = block_exponent(wave_max(tm)), eu = block_exponent(wave_max(tu));
+        const int em = block_exponent(block_top<WHOLE>(m, n)), eu = block_exponent(block_top<WHOLE>(u, n));
         const float dm = two_to(-em), du = two_to(-eu);
         const uint32_t id = (it.id + (uint32_t)at) * 0x9E3779B1u + s.salt;
         uint32_t cm = 0, cu = 0;
