@@ -417,7 +417,8 @@ int fp6_linear_v2_bf16(const uint16_t *X, int64_t M, const void *hi_plane, const
  *   rank    8 .. FP6_LORA_RANK_MAX, a multiple of 8 (adapters of a lower rank: rows of zeros); adapters 1 .. 65535
  *   workspace  >= fp6_lora_workspace_bytes; the contract of fp6_linear's workspace: its first FP6_WORKSPACE_ZERO_BYTES bytes are
  *           left as they are (so one buffer serves both), the rest need not be zero.  Calls that share it must not overlap in time.
- * fp6_lora_group: up to FP6_GROUP_MAX projections of the same rows (q, k and v; gate and up) in the same two launches; the rows'
+ * fp6_lora_group: up to FP6_GROUP_MAX projections of the same rows (q, k and v; gate and up) in the same two launches (more than 256
+ * rows: and one more for each projection); the rows'
  * adapters and the scaling are common, N, K and rank may differ.  No out may overlap what another layer of the group reads.
  * An infinity or NaN in a row of X stays in that row.  Errors: FP6_ERR_NULL, FP6_ERR_SHAPE (also M > 2^24, and sizes that need more
  * workgroups than a launch can have), FP6_ERR_ALIGN, FP6_ERR_VALUE (type,
@@ -463,7 +464,9 @@ int fp6_lora_backward(int type, const uint16_t *dY, const uint16_t *X, const flo
  *   scales_t     fp16 [K]: 2^E, the power of two at or above the largest S_n (at most 2^15)
  *   ratio        fp32 [N]: S_n / 2^E
  * fp6_linear_grad rounds dY * ratio to the type of dY, sums in fp32 and rounds the result: twice the rounding error of the result alone
- * in the mean square.  workspace: >= fp6_linear_grad_workspace_bytes, contract as for fp6_linear (its first
+ * in the mean square, sqrt(2) times its size.  fp16: products dY * ratio below 2^-14 are rounded in steps of 2^-24, so this holds for rows whose products
+ * are mostly above that; smaller gradients want a loss scale, the more so where one channel's scale stands far above the others' (ratios
+ * far below 1), or the bf16 format.  workspace: >= fp6_linear_grad_workspace_bytes, contract as for fp6_linear (its first
  * FP6_WORKSPACE_ZERO_BYTES bytes zero before first use, left zero).  FP6_ERR_VARIANT: another format.
  */
 int fp6_transpose_pack(int format, const void *hi_plane, const void *lo_plane, const uint16_t *scales, int64_t N, int64_t K,

@@ -248,7 +248,7 @@ __device__ __forceinline__ void step_block(const AdamwItem& it, int block, int l
 
 // A workgroup walks over the items of the plan; a wavefront takes the blocks of 256 elements wave, wave + 4, ... of an item, the next one's loads
 // in flight while it works on one.  Whole blocks take no branch; the last one of a tensor may be short.  Bound by memory: 109 million
-// elements with states in 8 bits 401 us for 1.96 GB, 4.9 TB/s (a large copy: 5.2), with 112 vector instructions an element beside it;
+// elements with states in 8 bits 397 us for 1.96 GB, 4.9 TB/s (a large copy: 5.2), with 126 vector instructions an element beside it;
 // 20 million with states in 32 bits 122 us, 4.9 TB/s; 0.6 million 6.8 us, of which a plan of one block takes 5.0.
 template <int BITS, typename G, typename C>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamwHeader* __restrict__ plan, const AdamwItem* __restrict__ list, int64_t items,

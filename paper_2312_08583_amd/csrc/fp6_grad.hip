@@ -68,7 +68,9 @@ __global__ __launch_bounds__(256) void turn_planes_kernel(const u32x4* __restric
 }
 
 // out = dY * ratio, rounded to the type of dY: the one rounding that the gradient has beside that of its result (with the scale inside the
-// sum a product of 11 + 11 bits has to become an operand of 11, or 8, bits on one side or the other).
+// sum a product of 11 + 11 bits has to become an operand of 11, or 8, bits on one side or the other).  In fp16 that holds down to 2^-14: the small products of
+// small gradients, or of channels far below the largest scale, lose bits as fp16 numbers of their size do.  Rows lifted by a power of two for the product and lowered
+// after it keep them, for a launch more in every call (16 x 4096 x 4096 13.0 us for 9.0): left to the caller's loss scale.
 // A thread keeps the ratios of its eight columns and walks down the rows: 2048 x 22016 30 us for 180 MB, 5.9 TB/s; a few rows 2.3 us, a launch.
 template <bool BF16>
 __global__ __launch_bounds__(256) void scale_rows_kernel(const u32x4* __restrict__ dY, const float4v* __restrict__ ratio, int64_t M,

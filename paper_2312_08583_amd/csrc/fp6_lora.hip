@@ -707,7 +707,7 @@ struct OuterLds : OuterW<JT, CT, FUSED> {
 // up per chunk; bf16: three terms.  Rows of other adapters count as zeros on both sides (an infinity in one of them does not reach this
 // sum), chunks without a row of this one are passed over.
 // Bound by the order of its steps, a chunk's loads, maxima, LDS and products, which two workgroups to a compute unit hide for each other: 4096 x 22016
-// rank 16 FUSED 54 us for 180 MB, 3.4 TB/s; rank 128 73 us for 2048 x 8192: P's terms out of LDS, read by every wavefront.
+// rank 16 FUSED 53 us for 180 MB, 3.4 TB/s; rank 128 69 us for 2048 x 8192: P's terms out of LDS, read by every wavefront.
 // FUSED: the chunk of Q in LDS is multiplied with W as well, S[block][m][j] = s * sum over the block's columns of Q[m][c] W[a][c][j]: the part of
 // a shrink that this block of columns has, so that Q is read once for both.
 template <int FMT, int JT, int CT, bool BY_COLUMN, bool FUSED>
