@@ -1,5 +1,6 @@
 """GPU: adapters and their gradients in every kernel that ranks and numbers of rows lead to, every element against the formula in 64 bits: ranks above 64
-and between 17 and 64 with few rows, with rows that pass 256 and 512, and with so many columns that more than 32 partial sums meet; groups of many rows."""
+and between 17 and 64 with few rows, with rows that pass 256 and 512, and with so many columns that more than 32 partial sums meet, or a workgroup
+takes 256 of them; groups of many rows."""
 import pytest
 import torch
 
@@ -24,6 +25,10 @@ CASES = [
     (1000, 8256, 320, 32, 3, "runs"),
     (1030, 192, 8256, 24, 1, "none"),
     (777, 448, 576, 32, 7, "mixed"),
+    (300, 192, 21888, 16, 3, "mixed"),    # 256 columns to a workgroup: with 128, three adapters on 171 blocks are more than 512
+    (300, 192, 21888, 24, 3, "runs"),
+    (300, 192, 21888, 40, 3, "mixed"),
+    (300, 21888, 192, 56, 3, "mixed"),
 ]
 
 
